@@ -241,7 +241,7 @@ def prepare(case, seed):
         s.limit = ints(_limits(case))
         s.row_of, s.cache_of, s.chunk_of = (ints(sum(([b] * r[i] for b, r in enumerate(reqs)), [])) for i in range(3))
         s.key_at = ints(sum((list(range(r[1])) for r in reqs), []) + sum((list(range(r[1], r[1] + r[2])) for r in reqs), []))
-        bounds = (len(reqs), max(r[0] for r in reqs), max(r[1] + r[2] for r in reqs))
+        bounds = (len(reqs), max(r[0] for r in reqs), max(r[1] for r in reqs) + max(r[2] for r in reqs))
     else:
         reqs = _requests(case)
         B, W = len(reqs), _pages_of(case)
