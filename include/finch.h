@@ -85,7 +85,7 @@ typedef enum { FINCH_GROUP_PER_KV_HEAD = 0, FINCH_GROUP_PER_LAYER = 1 } finch_gr
 enum {
     FINCH_DEV_BAD_BATCH = 1,   /* device-side batch metadata exceeds the host bounds given in finch_batch      */
     FINCH_DEV_TIMEOUT = 2,     /* a bounded wait inside a kernel ran out                                       */
-    FINCH_DEV_BAD_INDEX = 4    /* finch_compact met a kept index outside [0, N_b)                              */
+    FINCH_DEV_BAD_INDEX = 4    /* a kept index outside [0, N_b), a page number outside [0, n_pages)                */
 };
 
 typedef struct {
@@ -269,6 +269,109 @@ finch_status finch_step_host(finch_ctx *ctx, const void *host_prompt_q, const vo
                              const finch_tensor *out_v, int32_t *out_pos, int32_t *kept_idx, int32_t *out_len,
                              int32_t *host_kept_idx, int32_t *host_out_len, void *ws, size_t ws_bytes,
                              void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators around the step.  The paper's forward pass attends with chunk and prompt over [cache ; chunk] (Background, the
+ * attention equation) and then generates from the compressed cache ("Compression Output"); these calls do that part.
+ * They are forward passes only: nothing in this library learns.
+ *
+ *   finch_rotate         norms and positions of the queries and keys that a layer's projections give
+ *   finch_attend         attention of the prompt, or of chunk and prompt, over [cache ; chunk]; its row_lse over the prompt's own keys
+ *                        is the prompt_self_lse of finch_score
+ *   finch_pages_append   the compressed cache, and later each generated token, into a paged 8-bit cache
+ *   finch_pages_attend   attention of the newest tokens over it
+ *
+ * Conventions as above; besides, the context's device must be the current one (FINCH_ERR_INVALID_ARG otherwise), and a
+ * request whose device-side metadata exceeds the host bounds (FINCH_DEV_BAD_BATCH) has nothing written for it.
+ * Sums, softmax statistics and norms are fp32 in a fixed order: results are run-to-run identical.                       */
+
+/* Rotary positions: pair t of a row at position p turns by the angle p * inv_freq[t], formed with its cosine and sine in
+ * 64 bits; these are multiplied by `magnitude` and rounded to 32.  Plain host data: fill it with finch_rope_init.       */
+typedef struct {
+    int32_t rotary_dim;   /* leading coordinates of a head that turn: a multiple of 16, at most head_dim                  */
+    int32_t pairing;      /* 0: pairs (t, t + rotary_dim/2), 1: pairs (2t, 2t + 1), as finch_config.rope_pairing          */
+    float magnitude;      /* factor of cosine and sine, 1 unless a long-context scaling asks for another                  */
+    int32_t reserved;
+    double inv_freq[128]; /* [rotary_dim/2] angle per position                                                            */
+} finch_rope;
+
+/* inv_freq[t] = theta^(-2t/rotary_dim), [rotary_dim/2], stretched for contexts `factor` times as long as trained for:
+ *   FINCH_ROPE_PLAIN   not at all (factor and what follows are not read)
+ *   FINCH_ROPE_LINEAR  every frequency divided by factor
+ *   FINCH_ROPE_BASE    theta times factor^(rotary_dim / (rotary_dim - 2)): the slowest pair is stretched, the fastest kept
+ *   FINCH_ROPE_PARTS   a pair that turns n = original * f / 2 pi times within the `original` context keeps its frequency if
+ *                      n >= high, has it divided if n <= low, and blends the two linearly between
+ * Host arithmetic. FINCH_ERR_INVALID_ARG: an odd rotary_dim or one above 256, theta or factor below 1, low >= high ...   */
+enum { FINCH_ROPE_PLAIN = 0, FINCH_ROPE_LINEAR = 1, FINCH_ROPE_BASE = 2, FINCH_ROPE_PARTS = 3 };
+finch_status finch_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double original, double low,
+                                    double high, double *inv_freq);
+/* FINCH_ERR_UNSUPPORTED: rotary_dim is no multiple of 16. */
+finch_status finch_rope_init(finch_rope *out, int32_t rotary_dim, int32_t pairing, float magnitude, const double *inv_freq);
+
+/* For every row x of q ([n_layers][n_q_heads][tokens][head_dim]) and k ([n_layers][n_kv_heads][tokens][head_dim]):
+ *     y = x * rsqrt(mean(x^2) + eps) * weight     with q_weight / k_weight ([n_layers][head_dim], the context's dtype; NULL: y = x)
+ *     out = y turned to position pos[token]       with rope (NULL: out = y)
+ * in fp32, rounded once.  pos: device, [tokens] int32, any value, read only with rope.  A tensor with a null pointer (and a null output) is left
+ * out.  out_q / out_k may be q / k themselves (same pointer and strides); any other overlap is FINCH_ERR_INVALID_ARG.
+ * Neither rope nor weights: FINCH_ERR_INVALID_ARG. */
+finch_status finch_rotate(finch_ctx *ctx, const finch_tensor *q, const finch_tensor *k, int32_t tokens, const int32_t *pos,
+                          const finch_rope *rope, const void *q_weight, const void *k_weight, float eps, const finch_tensor *out_q,
+                          const finch_tensor *out_k, void *cuda_stream);
+
+/* Softmax attention of every packed query row over its request's candidates, [cache ; chunk]:
+ *     out[h,i] = sum_j exp(s[h,i,j] - lse[h,i]) v[kv(h),j],  s as in finch_score,  j < limit(i)
+ *   limit(i) = row_limit[i] clamped to [0, N_b] where the batch has row_limit; else, with causal = 1, N_b - n_q + i + 1 (the rows are the
+ *   request's last n_q tokens); else N_b.
+ * A row that sees nothing gives zeros and a log-sum-exp of -inf.  prompt_self_lse adds its term to the denominator (and to row_lse),
+ * as in finch_score.  `out` has q's shape and any strides; it must not overlap an input.  row_lse may be NULL.  budget is not read;
+ * row_norm must be 0.  bf16 with head_dim <= 128 runs on the tensor cores (P = exp(..) is rounded to bf16 there), everything else in
+ * fp32 multiply-adds.  What a row does not see is not read into its result where it lies behind the request's last candidate;
+ * a V row that is not finite, but is seen by some row of a request, may make rows before it not finite on the tensor cores.
+ * Workspace: finch_attend_workspace_bytes, enough for every batch with no larger total_q. */
+finch_status finch_attend_workspace_bytes(const finch_ctx *ctx, const finch_batch *batch, size_t *out);
+finch_status finch_attend(finch_ctx *ctx, const finch_tensor *q, const finch_tensor *cache_k, const finch_tensor *cache_v,
+                          const finch_tensor *chunk_k, const finch_tensor *chunk_v, const finch_batch *batch, int32_t causal,
+                          const finch_tensor *out, float *row_lse, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/* A paged cache in 8 bits.  Token t of request b lies in page table[b][t / 64], row t % 64, once that page is full: e4m3 codes with one
+ * scale for each page and KV head (value = code * scale, scale = largest finite magnitude / 448).  The tokens behind the last full page wait in
+ * the open rows of the request's slot, in the context's dtype: a page is quantised once, from unrounded rows, however they arrived.
+ * All arrays are dense device memory; codes and open rows 16-byte aligned.                                                    */
+enum { FINCH_PAGE_TOKENS = 64 };
+typedef struct {
+    void *k, *v;              /* [n_layers][n_pages][n_kv_heads][64][head_dim] e4m3                                        */
+    float *k_scale, *v_scale; /* [n_layers][n_pages][n_kv_heads]                                                           */
+    void *open_k, *open_v;    /* [n_layers][n_open][n_kv_heads][64][head_dim] context dtype                                */
+    const int32_t *table;     /* [batch][table_width] page numbers; entries of pages that are not full yet are not read    */
+    const int32_t *open_slot; /* [batch] in [0, n_open), or NULL: request b has slot b                                      */
+    int32_t n_pages, table_width, n_open;
+} finch_pages;
+
+typedef struct {
+    int32_t batch;
+    const int32_t *q_off;    /* device, [batch+1]: query rows (finch_pages_attend; else not read)                          */
+    const int32_t *new_off;  /* device, [batch+1]: new rows (finch_pages_append; else not read)                            */
+    const int32_t *len;      /* device, [batch]: tokens in the cache; for the append, before it                            */
+    int32_t total_q, total_new, max_q, max_new, max_len; /* host copies and upper bounds                                   */
+} finch_paged_batch;
+
+/* Appends rows [new_off[b], new_off[b+1]) of new_k / new_v ([n_layers][n_kv_heads][total_new][head_dim]) behind each request's len[b]
+ * tokens.  With rope, K rows turn to position pos[row] (device, [total_new]; NULL: len[b] + place among the new rows) and are
+ * rounded to the context's dtype once, before anything is quantised.  out_len (NULL, or [batch], apart from len) receives the new lengths.
+ * Pages and slots of different requests must be different.  Infinities are stored as the largest code, NaN as NaN; neither
+ * counts for the scale.  A page number outside [0, n_pages) sets FINCH_DEV_BAD_INDEX and its page is not written. */
+finch_status finch_pages_append(finch_ctx *ctx, const finch_pages *pages, const finch_paged_batch *batch, const finch_tensor *new_k,
+                                const finch_tensor *new_v, const finch_rope *rope, const int32_t *pos, int32_t *out_len,
+                                void *cuda_stream);
+
+/* out as finch_attend's, causal, over the cache's len[b] tokens: query row i of a request's n_q rows sees the first
+ * len[b] - n_q + i + 1.  Made for the last token, or the last few; every 8 rows of a KV head (its query heads times tokens)
+ * read the cache once.  Pages may be shared between requests.  A page number outside [0, n_pages) sets
+ * FINCH_DEV_BAD_INDEX and its tokens count as not there.  row_lse may be NULL.
+ * Workspace: finch_pages_workspace_bytes, enough for every batch with no larger total_q. */
+finch_status finch_pages_workspace_bytes(const finch_ctx *ctx, const finch_paged_batch *batch, size_t *out);
+finch_status finch_pages_attend(finch_ctx *ctx, const finch_pages *pages, const finch_paged_batch *batch, const finch_tensor *q,
+                                const finch_tensor *out, float *row_lse, void *ws, size_t ws_bytes, void *cuda_stream);
 
 /* Synchronises `cuda_stream`, copies the status word to *out (host) and clears it.  Returns FINCH_ERR_DEVICE_STATUS
  * when the word was non-zero, FINCH_ERR_CUDA when the stream reports an error. */

@@ -34,7 +34,8 @@ FINCH_DEV_BAD_BATCH, FINCH_DEV_TIMEOUT, FINCH_DEV_BAD_INDEX = 1, 2, 4
 
 EXPORTS = ("finch_ctx_create", "finch_ctx_destroy", "finch_workspace_bytes", "finch_score", "finch_select",
            "finch_compact", "finch_step", "finch_device_status", "finch_launch_count", "finch_status_string", "finch_score_static", "finch_score_static_max_rows", "finch_score_static_path",
-           "finch_step_host", "finch_score_plan")
+           "finch_step_host", "finch_score_plan", "finch_rope_frequencies", "finch_rope_init", "finch_rotate",
+           "finch_attend_workspace_bytes", "finch_attend", "finch_pages_append", "finch_pages_workspace_bytes", "finch_pages_attend")
 
 
 class finch_config(C.Structure):
@@ -56,6 +57,27 @@ class finch_batch(C.Structure):
                 ("max_cache", C.c_int32), ("max_chunk", C.c_int32), ("max_budget", C.c_int32),
                 ("prompt_self_lse", C.c_void_p), ("row_limit", C.c_void_p),
                 ("row_norm", C.c_int32)]
+
+
+FINCH_PAGE_TOKENS = 64
+FINCH_ROPE_PLAIN, FINCH_ROPE_LINEAR, FINCH_ROPE_BASE, FINCH_ROPE_PARTS = 0, 1, 2, 3
+
+
+class finch_rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("pairing", C.c_int32), ("magnitude", C.c_float), ("reserved", C.c_int32),
+                ("inv_freq", C.c_double * 128)]
+
+
+class finch_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("open_k", C.c_void_p), ("open_v", C.c_void_p), ("table", C.c_void_p), ("open_slot", C.c_void_p),
+                ("n_pages", C.c_int32), ("table_width", C.c_int32), ("n_open", C.c_int32)]
+
+
+class finch_paged_batch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("q_off", C.c_void_p), ("new_off", C.c_void_p), ("len", C.c_void_p),
+                ("total_q", C.c_int32), ("total_new", C.c_int32), ("max_q", C.c_int32), ("max_new", C.c_int32),
+                ("max_len", C.c_int32)]
 
 
 class FinchError(RuntimeError):
@@ -84,6 +106,15 @@ def load() -> C.CDLL:
         lib.finch_step.argtypes = [p] * 16 + [z, p]
         lib.finch_step_host.argtypes = [p] * 21 + [z, p]
         lib.finch_score_static.argtypes = [p] * 8
+        i, f, d = C.c_int32, C.c_float, C.c_double
+        lib.finch_rope_frequencies.argtypes = [i, d, i, d, d, d, d, p]
+        lib.finch_rope_init.argtypes = [p, i, i, f, p]
+        lib.finch_rotate.argtypes = [p, p, p, i, p, p, p, p, f, p, p, p]
+        lib.finch_attend_workspace_bytes.argtypes = [p] * 3
+        lib.finch_attend.argtypes = [p] * 7 + [i, p, p, p, z, p]
+        lib.finch_pages_append.argtypes = [p] * 9
+        lib.finch_pages_workspace_bytes.argtypes = [p] * 3
+        lib.finch_pages_attend.argtypes = [p] * 7 + [z, p]
         _lib = lib
     return _lib
 
@@ -304,3 +335,188 @@ def finch_step_host(ctx, host_prompt_q, host_chunk_k, host_chunk_v, host_chunk_p
         _ptr(stage_chunk_pos), v + 3 * z, v + 4 * z, _ptr(cache_pos), C.addressof(batch.c), v + 5 * z, v + 6 * z,
         _ptr(out_pos), _ptr(kept_idx), _ptr(out_len), _ptr(host_kept_idx), _ptr(host_out_len), _ptr(ws), _nbytes(ws),
         _stream(stream)), "finch_step_host")
+
+
+# ------------------------------------------------------------------ rotation, attention, the paged 8-bit cache
+
+def _same(what: str, like, *tensors) -> None:
+    """Every tensor on `like`'s device and of its dtype: a kernel would read the bits of another one all the same."""
+    for t in tensors:
+        if t is not None and (t.dtype != like.dtype or t.device != like.device):
+            raise ValueError(f"{what}: expected {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+
+
+def _typed(what: str, dtype: str, like, *tensors) -> None:
+    for t in tensors:
+        if t is not None and (str(t.dtype) != "torch." + dtype or t.device != like.device or not t.is_contiguous()):
+            raise ValueError(f"{what}: expected a contiguous torch.{dtype} tensor on {like.device}, got {t.dtype} on {t.device}")
+
+
+def _shape(what: str, t, shape) -> None:
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def finch_rope_frequencies(rotary_dim: int, theta: float = 10000.0, scaling: int = FINCH_ROPE_PLAIN, factor: float = 1.0,
+                           original: float = 8192.0, low: float = 1.0, high: float = 4.0):
+    """Angle per position of every pair, float64 [rotary_dim / 2] (see the header for the scalings)."""
+    out = np.zeros(max(rotary_dim // 2, 1), dtype=np.float64)
+    _check(load().finch_rope_frequencies(rotary_dim, theta, scaling, factor, original, low, high, out.ctypes.data),
+           "finch_rope_frequencies")
+    return out
+
+
+def finch_rope_init(rotary_dim: int, inv_freq, pairing: int = 0, magnitude: float = 1.0) -> finch_rope:
+    freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    if freq.shape != (rotary_dim // 2,):
+        raise ValueError(f"expected {rotary_dim // 2} frequencies, got shape {freq.shape}")
+    rope = finch_rope()
+    _check(load().finch_rope_init(C.addressof(rope), rotary_dim, pairing, magnitude, freq.ctypes.data), "finch_rope_init")
+    return rope
+
+
+def _rope(rope) -> Optional[int]:
+    return None if rope is None else C.addressof(rope)
+
+
+def finch_rotate(ctx, q, k, pos, out_q, out_k, rope: Optional[finch_rope] = None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 stream=None) -> None:
+    """Norm (with weights) and rotation (with rope and positions) of q and k, [n_layers][heads][tokens][head_dim]; either may be
+    None, together with its output."""
+    like = q if q is not None else k
+    if like is None:
+        raise ValueError("finch_rotate: neither q nor k")
+    _same("finch_rotate", like, q, k, out_q, out_k, q_weight, k_weight)
+    _typed("finch_rotate: pos", "int32", like, pos)
+    L, _, tokens, d = like.shape
+    for x, out, w in ((q, out_q, q_weight), (k, out_k, k_weight)):
+        if (x is None) != (out is None):
+            raise ValueError("finch_rotate: a tensor and its output come together")
+        if x is not None:
+            _shape("finch_rotate", x, (L, x.shape[1], tokens, d))
+            _shape("finch_rotate: output", out, x.shape)
+        if w is not None and not w.is_contiguous():
+            raise ValueError("finch_rotate: weights are contiguous [n_layers][head_dim]")
+        _shape("finch_rotate: weight", w, (L, d))
+    if pos is not None:
+        _shape("finch_rotate: pos", pos, (tokens,))
+    keep, v = _views(q, k, out_q, out_k)
+    z = _VIEW_BYTES
+    _check(load().finch_rotate(ctx, v, v + z, tokens, _ptr(pos), _rope(rope), _ptr(q_weight), _ptr(k_weight), eps, v + 2 * z,
+                               v + 3 * z, _stream(stream)), "finch_rotate")
+
+
+def finch_attend_workspace_bytes(ctx, batch: Batch) -> int:
+    out = C.c_size_t()
+    _check(load().finch_attend_workspace_bytes(ctx, C.addressof(batch.c), C.addressof(out)), "finch_attend_workspace_bytes")
+    return int(out.value)
+
+
+def finch_attend(ctx, q, cache_k, cache_v, chunk_k, chunk_v, batch: Batch, out, row_lse=None, causal: bool = True, ws=None,
+                 stream=None) -> None:
+    """Attention of the packed query rows over [cache ; chunk] (see the header); `out` has q's shape."""
+    _same("finch_attend", q, cache_k, cache_v, chunk_k, chunk_v, out)
+    _typed("finch_attend: row_lse", "float32", q, row_lse)
+    _shape("finch_attend: out", out, q.shape)
+    _shape("finch_attend: row_lse", row_lse, q.shape[:3])
+    keep, v = _views(q, cache_k, cache_v, chunk_k, chunk_v, out)
+    z = _VIEW_BYTES
+    _check(load().finch_attend(ctx, v, v + z, v + 2 * z, v + 3 * z, v + 4 * z, C.addressof(batch.c), int(bool(causal)), v + 5 * z,
+                               _ptr(row_lse), _ptr(ws), _nbytes(ws), _stream(stream)), "finch_attend")
+
+
+@dataclass
+class Pages:
+    """The tensors of a paged cache and the finch_pages that describes them."""
+    tensors: tuple
+    c: finch_pages
+
+
+def make_pages(k, v, k_scale, v_scale, open_k, open_v, table, open_slot=None) -> Pages:
+    """k, v: uint8 [n_layers][n_pages][n_kv_heads][64][head_dim]; scales: float32 [n_layers][n_pages][n_kv_heads]; open_k, open_v:
+    [n_layers][n_open][n_kv_heads][64][head_dim] in the context's dtype; table: int32 [batch][table_width]; open_slot: int32 [batch]."""
+    import torch
+    L, n_pages, Hkv, page, d = k.shape
+    n_open = open_k.shape[1]
+    for name, t, dtype, shape in (("k", k, torch.uint8, k.shape), ("v", v, torch.uint8, k.shape),
+                                  ("k_scale", k_scale, torch.float32, (L, n_pages, Hkv)),
+                                  ("v_scale", v_scale, torch.float32, (L, n_pages, Hkv)),
+                                  ("open_k", open_k, open_k.dtype, (L, n_open, Hkv, page, d)),
+                                  ("open_v", open_v, open_k.dtype, (L, n_open, Hkv, page, d)),
+                                  ("table", table, torch.int32, (table.shape[0], table.shape[-1])),
+                                  ("open_slot", open_slot, torch.int32, (table.shape[0],))):
+        if t is None and name == "open_slot":
+            continue
+        if t.dtype != dtype or t.device != k.device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+            raise ValueError(f"make_pages: {name} is to be contiguous {dtype} {tuple(shape)} on {k.device}, got {t.dtype} {tuple(t.shape)}")
+    if page != FINCH_PAGE_TOKENS:
+        raise ValueError(f"make_pages: a page has {FINCH_PAGE_TOKENS} tokens, got {page}")
+    tensors = (k, v, k_scale, v_scale, open_k, open_v, table, open_slot)
+    return Pages(tensors, finch_pages(*map(_ptr, tensors), n_pages, table.shape[1], n_open))
+
+
+@dataclass
+class PagedBatch:
+    """Device-side metadata of a call on a paged cache plus the host bounds finch_paged_batch carries."""
+    q_off: object
+    new_off: object
+    len: object
+    c: finch_paged_batch
+
+    @property
+    def batch(self) -> int:
+        return self.c.batch
+
+
+def make_paged_batch(lengths: Sequence[int], q_off: Optional[Sequence[int]] = None, new_off: Optional[Sequence[int]] = None,
+                     device="cuda", len_tensor=None, max_len: Optional[int] = None) -> PagedBatch:
+    """lengths: tokens of each request in the cache (for an append, before it).  len_tensor: a device tensor that holds them
+    instead (a length that an earlier append wrote), with max_len as the bound on them."""
+    import torch
+    h = np.ascontiguousarray(lengths, dtype=np.int32)
+    B = len(h)
+    d_len = torch.from_numpy(h).to(device) if len_tensor is None else len_tensor
+    if d_len.dtype != torch.int32 or not d_len.is_contiguous() or d_len.numel() < B:
+        raise ValueError("make_paged_batch: lengths are contiguous int32, one for each request")
+    offs = []
+    for off in (q_off, new_off):
+        if off is None:
+            offs.append((None, 0, 0))
+            continue
+        o = np.ascontiguousarray(off, dtype=np.int32)
+        assert len(o) == B + 1
+        offs.append((torch.from_numpy(o).to(device), int(o[B]), int(np.diff(o).max()) if B else 0))
+    longest = (int(h.max()) if B else 0) if max_len is None else int(max_len)
+    c = finch_paged_batch(B, _ptr(offs[0][0]), _ptr(offs[1][0]), _ptr(d_len), offs[0][1], offs[1][1], offs[0][2], offs[1][2], longest)
+    return PagedBatch(offs[0][0], offs[1][0], d_len, c)
+
+
+def finch_pages_append(ctx, pages: Pages, batch: PagedBatch, new_k, new_v, out_len=None, rope: Optional[finch_rope] = None, pos=None,
+                       stream=None) -> None:
+    """Rows of new_k (turned to their positions with rope) and new_v behind each request's tokens (see the header)."""
+    _same("finch_pages_append", pages.tensors[4], new_k, new_v)
+    _typed("finch_pages_append: out_len and pos", "int32", new_k, out_len, pos)
+    if pos is not None:
+        _shape("finch_pages_append: pos", pos, (new_k.shape[2],))
+    if out_len is not None and out_len.numel() < batch.c.batch:
+        raise ValueError("finch_pages_append: out_len holds a length for each request")
+    keep, v = _views(new_k, new_v)
+    _check(load().finch_pages_append(ctx, C.addressof(pages.c), C.addressof(batch.c), v, v + _VIEW_BYTES, _rope(rope), _ptr(pos),
+                                     _ptr(out_len), _stream(stream)), "finch_pages_append")
+
+
+def finch_pages_workspace_bytes(ctx, batch: PagedBatch) -> int:
+    out = C.c_size_t()
+    _check(load().finch_pages_workspace_bytes(ctx, C.addressof(batch.c), C.addressof(out)), "finch_pages_workspace_bytes")
+    return int(out.value)
+
+
+def finch_pages_attend(ctx, pages: Pages, batch: PagedBatch, q, out, row_lse=None, ws=None, stream=None) -> None:
+    """Attention of each request's newest tokens over its paged cache (see the header); `out` has q's shape."""
+    _same("finch_pages_attend", pages.tensors[4], q, out)
+    _typed("finch_pages_attend: row_lse", "float32", q, row_lse)
+    _shape("finch_pages_attend: out", out, q.shape)
+    _shape("finch_pages_attend: row_lse", row_lse, q.shape[:3])
+    keep, v = _views(q, out)
+    _check(load().finch_pages_attend(ctx, C.addressof(pages.c), C.addressof(batch.c), v, v + _VIEW_BYTES, _ptr(row_lse), _ptr(ws),
+                                     _nbytes(ws), _stream(stream)), "finch_pages_attend")

@@ -1,0 +1,460 @@
+// Attention of packed query rows over [cache ; chunk] on the tensor cores (bf16, head dimensions up to 128).
+//
+//   S = Q K^T, O = softmax(S) V, a row's softmax over its first `limit` candidates, by the online recurrence over key tiles:
+//   m' = max(m, max S), O = O 2^(m - m') + P V with P = 2^(S - m'), l = l 2^(m - m') + sum P.
+//
+// Rows.  A tile is 128 rows of one KV head: all its query heads (they share every key) times as many tokens as fit, row =
+// head * tok + token, which is how one TMA box lays them out.  Keys come in tiles of 128 that do not straddle the cache / chunk seam.
+//
+// Streams.  A CTA works on two streams at a time, a softmax warpgroup each, so that the tensor core multiplies for one while the other
+// exponentiates: two row tiles against the same keys, or, for requests of a single row tile, one row tile against the even and
+// the odd key tiles (whose results are added through shared memory at the end).
+//
+// Tensor memory (512 columns): S of each stream (128), over whose first half P is written as bf16, and O of each stream.  P never leaves
+// tensor memory: it is the A operand of P V.  V tiles are B operands with their rows along K.
+// Order.  One thread issues S(s, i+1) behind P V (s, i): the completion of S then says that O is at rest, and the softmax warps
+// may scale it.  They do so only when a row's maximum has grown by more than 2^8: until then P is taken against the old reference.
+//
+// A masked key has P = 0, but zero times a NaN or infinity is none: rows of V behind the last candidate are cleared before
+// they are multiplied.
+#include "attend.cuh"
+
+namespace finch {
+namespace {
+
+using namespace ptx;
+using namespace tc;
+
+constexpr int kTcThreads = 384;      // 4 control warps, 2 x 4 softmax warps
+constexpr float kGrowth = 8.f;       // binary orders that a row's maximum may grow before O is scaled
+constexpr int kTileRows = 128;
+
+struct TcArgs {
+    ModelView mv;
+    BatchView bv;
+    AttendOut out;
+    int *status;
+    int causal, heads, tok, chunks, row_tiles;  // query heads and tokens of a row tile; tiles of heads per KV head; CTAs along the tokens
+    int two_tiles;                               // streams are two row tiles (else: one tile's even and odd key tiles)
+    float scale2;
+};
+
+struct Maps {
+    CUtensorMap q, ck, cv, hk, hv;
+};
+
+template <int DP>
+struct Layout {
+    static constexpr int kSlabs = DP / 64;
+    static constexpr int kTile = kSlabs * kSlabBytes;
+    static constexpr int kStages = DP == 128 ? 5 : 8;
+    static constexpr int kBytes = (2 + kStages) * kTile + 1024;
+};
+
+struct Barriers {
+    uint64_t q_full, full[8], empty[8], s_full[2], p_full[2], o_full[2];
+    uint64_t ragged[2], clean[2];  // the cache's, the chunk's last V tile: on its way, cleared behind its rows
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TcArgs p) {
+    using Lay = Layout<DP>;
+    extern __shared__ uint8_t raw[];
+    __shared__ Barriers bar;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    __shared__ int limit_s[2];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    uint8_t *q_smem = smem, *ring = smem + 2 * Lay::kTile;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    dependency_wait();
+    const ModelView &mv = p.mv;
+    const int b = blockIdx.y;
+    int x = blockIdx.x;
+    const int split = x % p.out.splits;
+    x /= p.out.splits;
+    const int hc = x % p.chunks;
+    x /= p.chunks;
+    const int kvh = x % mv.Hkv, l = x / mv.Hkv % mv.L, tile = p.row_tiles - 1 - x / mv.Hkv / mv.L;  // long causal rows first
+    const UnitInfo u = unit_info(mv, p.bv, 0, b);
+    if (!u.ok) {
+        if (threadIdx.x == 0) atomicOr(p.status, FINCH_DEV_BAD_BATCH);
+        return;
+    }
+    const int t0 = tile * (p.two_tiles ? 2 : 1) * p.tok;
+    if (t0 >= u.n_q) return;
+    const int h0 = kvh * mv.g + hc * p.heads, n_heads = min(p.heads, mv.g - hc * p.heads);
+
+    // ---- set-up; how many candidates the rows of each stream see at most
+    if (warp == 0) {
+        if (lane == 0) {
+            mbar_init(&bar.q_full, 1);
+            for (int i = 0; i < Lay::kStages; ++i) mbar_init(&bar.full[i], 1), mbar_init(&bar.empty[i], 1);
+            for (int i = 0; i < 2; ++i)
+                mbar_init(&bar.s_full[i], 1), mbar_init(&bar.p_full[i], 4), mbar_init(&bar.o_full[i], 1), mbar_init(&bar.ragged[i], 1), mbar_init(&bar.clean[i], 1);
+            abort_flag = 0;
+            fence_barrier_init();
+        }
+    } else if (warp == 1) {
+        tmem_alloc(&tmem_slot, 512);
+        tmem_relinquish();
+    } else {
+        const int s = warp - 2;
+        if (s < 2) {
+            int most = 0;
+            const int ts = t0 + (p.two_tiles ? s * p.tok : 0);
+            for (int i = lane; i < p.tok; i += 32)
+                if (ts + i < u.n_q) most = max(most, attend_limit(p.bv, u, ts + i, p.causal));
+            most = __reduce_max_sync(0xffffffffu, most);
+            if (lane == 0) limit_s[s] = most;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    // ---- key tiles of the CTA's split and of each stream
+    const int cache_tiles = (u.c + kTileRows - 1) / kTileRows;
+    auto tiles_for = [&](int limit) {
+        return limit <= u.c ? (limit + kTileRows - 1) / kTileRows : cache_tiles + (limit - u.c + kTileRows - 1) / kTileRows;
+    };
+    const int all0 = tiles_for(limit_s[0]), all1 = tiles_for(limit_s[1]), all = max(all0, all1);
+    const int begin = (int)((int64_t)all * split / p.out.splits), end = (int)((int64_t)all * (split + 1) / p.out.splits);
+    const int n_tiles = end - begin;                    // loaded
+    int count[2];                                        // of each stream
+    if (p.two_tiles) {
+        count[0] = max(0, min(end, all0) - begin), count[1] = max(0, min(end, all1) - begin);
+    } else {
+        count[0] = (n_tiles + 1) / 2, count[1] = n_tiles / 2;
+    }
+    auto tile_of = [&](int s, int i) { return p.two_tiles ? i : 2 * i + s; };  // in the split
+    // the last stream to use a tile frees it
+    auto frees = [&](int s, int t) { return !p.two_tiles || s == 1 || t >= count[1]; };
+    constexpr int kStages = Lay::kStages;
+    const uint32_t s_col[2] = {tmem, tmem + 128}, o_col[2] = {tmem + 256, tmem + 256 + DP};
+
+    if (warp < 4) regs_dec<56>();
+    if (warp == 0) {
+        // ---------------------------------------------------------------- producer
+        if (lane == 0 && n_tiles > 0) {
+            const int q_tiles = p.two_tiles ? 2 : 1;
+            mbar_expect_tx(&bar.q_full, q_tiles * Lay::kSlabs * p.tok * p.heads * 128);
+            for (int s = 0; s < q_tiles; ++s)
+                for (int c = 0; c < Lay::kSlabs; ++c)
+                    tma_load_4d(q_smem + s * Lay::kTile + c * kSlabBytes, &maps.q, &bar.q_full, c * 64, u.q0 + t0 + s * p.tok, h0, l);
+            int item = 0;
+            bool ok = true;
+            for (int t = 0; t < n_tiles && ok; ++t) {
+                const KeyTile kt = key_tile(u, begin + t);
+                for (int v = 0; v < 2; ++v, ++item) {
+                    const int slot = item % kStages;
+                    if (item >= kStages && !(ok = mbar_wait(&bar.empty[slot], (item / kStages - 1) & 1, &abort_flag))) break;
+                    mbar_expect_tx(&bar.full[slot], Lay::kTile);
+                    const CUtensorMap *map = kt.is_chunk ? (v ? &maps.hv : &maps.hk) : (v ? &maps.cv : &maps.ck);
+                    for (int c = 0; c < Lay::kSlabs; ++c)
+                        tma_load_4d(ring + slot * Lay::kTile + c * kSlabBytes, map, &bar.full[slot], c * 64, kt.row0, kvh, l);
+                    if (v && kt.valid < kTileRows) mbar_arrive(&bar.ragged[kt.is_chunk]);
+                }
+            }
+            // no copy of this CTA is in flight when its shared memory goes to another
+            mbar_wait(&bar.q_full, 0, &abort_flag);
+            for (int i = max(0, item - kStages); i < item; ++i) mbar_wait(&bar.full[i % kStages], (i / kStages) & 1, &abort_flag);
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- MMA issuer
+        if (lane == 0 && n_tiles > 0) {
+            constexpr uint32_t idesc_s = idesc_bf16_f32(128, 128), idesc_o = idesc_bf16_f32(128, DP) | kIdescBMn;
+            bool ok = mbar_wait(&bar.q_full, 0, &abort_flag);
+            const uint32_t ring_u = smem_u32(ring), q_u = smem_u32(q_smem);
+            auto issue_s = [&](int s, int i) {
+                const int t = tile_of(s, i), item = 2 * t, slot = item % kStages;
+                if (!mbar_wait(&bar.full[slot], (item / kStages) & 1, &abort_flag)) return false;
+                tc_fence_after();
+                const uint32_t qa = q_u + (p.two_tiles ? s : 0) * Lay::kTile, ka = ring_u + slot * Lay::kTile;
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    const uint32_t at = (k / 4) * kSlabBytes + (k % 4) * 32;
+                    if (k == 0)
+                        umma_bf16_first(s_col[s], smem_desc_sw128(qa + at), smem_desc_sw128(ka + at), idesc_s);
+                    else
+                        umma_bf16_acc(s_col[s], smem_desc_sw128(qa + at), smem_desc_sw128(ka + at), idesc_s);
+                }
+                umma_commit(&bar.s_full[s]);
+                if (frees(s, t)) umma_commit(&bar.empty[slot]);
+                return true;
+            };
+            auto issue_o = [&](int s, int i) {
+                const int t = tile_of(s, i), item = 2 * t + 1, slot = item % kStages;
+                if (!mbar_wait(&bar.p_full[s], i & 1, &abort_flag)) return false;
+                if (!mbar_wait(&bar.full[slot], (item / kStages) & 1, &abort_flag)) return false;
+                const KeyTile kt = key_tile(u, begin + t);
+                if (kt.valid < kTileRows && !mbar_wait(&bar.clean[kt.is_chunk], 0, &abort_flag)) return false;
+                tc_fence_after();
+                const uint32_t va = ring_u + slot * Lay::kTile;
+#pragma unroll
+                for (int k = 0; k < kTileRows / 16; ++k)
+                    umma_bf16_tmem(o_col[s], s_col[s] + k * 8, smem_desc_sw128_mn(va + k * 2048, kSlabBytes), idesc_o, i > 0 || k > 0);
+                if (frees(s, t)) umma_commit(&bar.empty[slot]);
+                if (i + 1 == count[s]) umma_commit(&bar.o_full[s]);
+                return true;
+            };
+            for (int s = 0; s < 2 && ok; ++s)
+                if (count[s] > 0) ok = issue_s(s, 0);
+            for (int i = 0; ok && i < max(count[0], count[1]); ++i)
+                for (int s = 0; s < 2 && ok; ++s) {
+                    if (i < count[s]) ok = issue_o(s, i);
+                    if (ok && i + 1 < count[s]) ok = issue_s(s, i + 1);
+                }
+        }
+    } else if (warp == 2) {
+        // ---------------------------------------------------------------- V rows behind the last candidate
+        for (int t = 0; t < n_tiles; ++t) {
+            const KeyTile kt = key_tile(u, begin + t);
+            if (kt.valid == kTileRows) continue;
+            const int item = 2 * t + 1, slot = item % kStages;
+            // this warp has not seen the slot's earlier phases: it waits until the slot is this tile's, then for its bytes
+            if (!__all_sync(0xffffffffu, mbar_wait_relaxed(&bar.ragged[kt.is_chunk], 0, &abort_flag, 200) &&
+                                             mbar_wait(&bar.full[slot], (item / kStages) & 1, &abort_flag)))
+                break;
+            for (int i = lane; i < (kTileRows - kt.valid) * 8; i += 32)
+#pragma unroll
+                for (int c = 0; c < Lay::kSlabs; ++c)
+                    *(uint4 *)(ring + slot * Lay::kTile + c * kSlabBytes + kt.valid * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.clean[kt.is_chunk]);
+        }
+    } else if (warp >= 4) {
+        // ---------------------------------------------------------------- softmax
+        regs_inc<224>();
+        const int s = (warp - 4) / 4, quarter = warp % 4, r = quarter * 32 + lane;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t st = s_col[s] + lane_base, ot = o_col[s] + lane_base;
+        const int hr = r / p.tok, tr = t0 + (p.two_tiles ? s * p.tok : 0) + r % p.tok;
+        const bool live = hr < n_heads && tr < u.n_q;
+        const int limit = live ? attend_limit(p.bv, u, tr, p.causal) : INT_MAX;
+        const float growth = kGrowth / p.scale2;
+        float m = -INFINITY, sum = 0.f;
+        bool ok = true;
+        for (int i = 0; i < count[s]; ++i) {
+            const KeyTile kt = key_tile(u, begin + tile_of(s, i));
+            const int nv = min(limit - kt.j0, kt.valid);   // columns that this row sees
+            if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar.s_full[s], i & 1, &abort_flag)))) break;
+            tc_fence_after();
+            uint32_t v[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_issue(st + c * 32, v[c]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_wait(v[c]);
+            if (__any_sync(0xffffffffu, nv < kTileRows)) {
+                keep_branch();
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (c * 32 + e >= nv) v[c][e] = 0xff800000u;  // -inf
+            }
+            float top = fmaxf(fmaxf(chunk_max(v[0]), chunk_max(v[1])), fmaxf(chunk_max(v[2]), chunk_max(v[3])));
+            if (__any_sync(0xffffffffu, live && top > m + growth)) {  // always at the first tile
+                keep_branch();
+                if (i > 0) {
+                    const float now = top > m + growth ? top : m;
+                    const float f = now == m ? 1.f : ex2((m - now) * p.scale2);
+                    sum *= f;
+                    m = now;
+#pragma unroll 1
+                    for (int c = 0; c < DP / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_ld_issue(ot + c * 32, o);
+                        tmem_ld_wait(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st(ot + c * 32, o);
+                    }
+                    tmem_st_wait();
+                } else {
+                    m = top;
+                }
+            }
+            const float negm = m == -INFINITY ? 0.f : -(m * p.scale2);
+            const uint64_t s2 = pack2(p.scale2, p.scale2), n2 = pack2(negm, negm);
+            uint64_t acc0 = 0, acc1 = 0;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t w[32];
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    const uint32_t *src = &v[2 * c + e / 16][e % 16 * 2];
+                    const uint64_t a = exp2_pair(fma2(pack2(__uint_as_float(src[0]), __uint_as_float(src[1])), s2, n2));
+                    const uint64_t d = exp2_pair(fma2(pack2(__uint_as_float(src[2]), __uint_as_float(src[3])), s2, n2));
+                    acc0 = add2(acc0, a);
+                    acc1 = add2(acc1, d);
+                    float a0, a1, d0, d1;
+                    unpack2(a, a0, a1);
+                    unpack2(d, d0, d1);
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[e]) : "f"(a1), "f"(a0));
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[e + 1]) : "f"(d1), "f"(d0));
+                }
+                tmem_st(st + c * 32, w);
+            }
+            sum += sum_of(acc0, acc1);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.p_full[s]);
+        }
+        // ---- the row's result
+        if (count[s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.o_full[s], 0, &abort_flag));
+        tc_fence_after();
+        const float m2 = m * p.scale2;   // the reference in base-2 logits (-inf: none of the row's keys)
+        const int64_t row = live ? attend_row(mv, p.bv.total_q, l, h0 + hr, u.q0 + tr) : 0;
+        float scale_o = 1.f, total = sum, ref = m2, other = 0.f;
+        float *swap = (float *)ring;     // [DP + 2][128]: the second stream's O, m, l
+        bool writes = live;
+        if (!p.two_tiles && count[1] > 0) {
+            // every MMA that reads the ring is complete before the second stream's result goes there
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.o_full[1 - s], 0, &abort_flag));
+            if (s == 1) {
+#pragma unroll 1
+                for (int c = 0; c < DP / 32; ++c) {
+                    uint32_t o[32];
+                    tmem_ld_issue(ot + c * 32, o);
+                    tmem_ld_wait(o);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) swap[(c * 32 + e) * 128 + r] = __uint_as_float(o[e]);
+                }
+                swap[DP * 128 + r] = m2;
+                swap[(DP + 1) * 128 + r] = sum;
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (s == 0) {
+                const float mo = swap[DP * 128 + r], lo = swap[(DP + 1) * 128 + r];
+                ref = fmaxf(sum == 0.f ? -INFINITY : m2, lo == 0.f ? -INFINITY : mo);
+                const float base = ref == -INFINITY ? 0.f : ref;
+                scale_o = sum == 0.f ? 0.f : exp2f(m2 - base);
+                other = lo == 0.f ? 0.f : exp2f(mo - base);
+                total = sum * scale_o + lo * other;
+            }
+        }
+        if (!p.two_tiles && s == 1) writes = false;
+        float lse = 0.f, inv = 1.f;
+        const bool partial = p.out.splits > 1;
+        if (writes && !partial) inv = attend_finish(ref, total, p.bv.self_lse, row, lse);
+        const int64_t slot = split * ((int64_t)mv.L * mv.Hq * p.bv.total_q) + row;
+        __nv_bfloat16 *dst = (__nv_bfloat16 *)p.out.ptr + (int64_t)l * p.out.stride_layer + (int64_t)(h0 + hr) * p.out.stride_head +
+                             (int64_t)(u.q0 + tr) * p.out.stride_tok;
+#pragma unroll 1
+        for (int c = 0; c < mv.d / 32 && (p.two_tiles || s == 0); ++c) {
+            uint32_t o[32];
+            if (count[s] > 0) {
+                tmem_ld_issue(ot + c * 32, o);
+                tmem_ld_wait(o);
+            }
+            float y[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                y[e] = count[s] > 0 && sum != 0.f ? __uint_as_float(o[e]) * scale_o : 0.f;
+                if (other != 0.f) y[e] = fmaf(swap[(c * 32 + e) * 128 + r], other, y[e]);
+                y[e] *= inv;
+            }
+            if (writes && partial) {
+                float *po = p.out.part_o + slot * mv.d + c * 32;
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) *(float4 *)(po + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+            } else if (writes) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(y[e + 2 * k + 1]), "f"(y[e + 2 * k]));
+                    *(uint4 *)(dst + c * 32 + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            __syncwarp();
+        }
+        if (writes) {
+            if (partial)
+                p.out.part_ml[slot] = make_float2(ref, total);
+            else if (p.out.row_lse)
+                p.out.row_lse[row] = lse;
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+    if (threadIdx.x == 0 && abort_flag) atomicOr(p.status, FINCH_DEV_TIMEOUT);
+}
+
+template <int DP>
+cudaError_t launch(const Ctx &ctx, const Maps &maps, const TcArgs &p, dim3 grid, cudaStream_t stream) {
+    const int bit = kSmemAttendTc + (DP == 128);
+    if (!ctx.smem_ready(bit)) {
+        cudaError_t e = cudaFuncSetAttribute(attend_tc_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<DP>::kBytes);
+        if (e != cudaSuccess) return e;
+        ctx.smem_set(bit);
+    }
+    ctx.launches += 1;
+    return launch_chained(attend_tc_kernel<DP>, grid, dim3(kTcThreads), Layout<DP>::kBytes, stream, maps, p);
+}
+
+// A map of a row tile's queries: one box is `tok` tokens of `heads` heads.
+bool make_q_map(CUtensorMap *map, const TensorView &t, int d, int64_t tokens, int heads, int layers, int tok, int box_heads) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn || !t.ptr || tokens <= 0) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)layers};
+    const cuuint64_t strides[3] = {(cuuint64_t)t.stride_tok * 2, (cuuint64_t)t.stride_head * 2, (cuuint64_t)t.stride_layer * 2};
+    for (int i = 0; i < 3; ++i)
+        if (strides[i] == 0 || strides[i] % 16 || strides[i] >= (1ull << 40)) return false;
+    const cuuint32_t box[4] = {64, (cuuint32_t)tok, (cuuint32_t)box_heads, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<char *>(t.ptr), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+bool attend_tc_supported(const Ctx &ctx) { return ctx.cfg.dtype == FINCH_BF16 && ctx.model.d <= 128; }
+
+cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorView &ck, const TensorView &cv, const TensorView &hk,
+                             const TensorView &hv, const BatchView &bv, int causal, AttendOut out, size_t partial_rows, cudaStream_t stream) {
+    if (bv.batch == 0 || bv.max_q == 0) return cudaSuccess;
+    const ModelView &mv = ctx.model;
+    TcArgs p = {mv, bv, out, ctx.d_status, causal, 0, 0, 0, 0, 0, mv.scale * kLog2e};
+    p.heads = mv.g < kTileRows ? mv.g : kTileRows;
+    p.tok = kTileRows / p.heads;
+    p.chunks = (mv.g + p.heads - 1) / p.heads;
+    p.two_tiles = bv.max_q > p.tok;
+    const int per_cta = p.two_tiles ? 2 * p.tok : p.tok;
+    p.row_tiles = (bv.max_q + per_cta - 1) / per_cta;
+    Maps maps;
+    if (!make_q_map(&maps.q, q, mv.d, bv.total_q, mv.Hq, mv.L, p.tok, p.heads)) return cudaErrorNotSupported;
+    // an absent tensor holds no tile; its map is never used
+    const bool cache = bv.total_cache > 0 && ck.ptr && cv.ptr, chunk = bv.total_chunk > 0 && hk.ptr && hv.ptr;
+    if (cache && (!make_map(&maps.ck, ck, mv.d, bv.total_cache, mv.Hkv, mv.L, kTileRows) ||
+                  !make_map(&maps.cv, cv, mv.d, bv.total_cache, mv.Hkv, mv.L, kTileRows)))
+        return cudaErrorNotSupported;
+    if (chunk && (!make_map(&maps.hk, hk, mv.d, bv.total_chunk, mv.Hkv, mv.L, kTileRows) ||
+                  !make_map(&maps.hv, hv, mv.d, bv.total_chunk, mv.Hkv, mv.L, kTileRows)))
+        return cudaErrorNotSupported;
+    if (!cache) maps.ck = maps.cv = maps.q;
+    if (!chunk) maps.hk = maps.hv = maps.q;
+    const int64_t units = (int64_t)mv.L * mv.Hkv * p.chunks;
+    const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
+    const int key_tiles = (bv.max_cache + kTileRows - 1) / kTileRows + (bv.max_chunk + kTileRows - 1) / kTileRows;
+    int splits = attend_splits(units * p.row_tiles * bv.batch, ctx.sm_count, key_tiles, 2);
+    while (splits > 1 && splits * rows > partial_rows) --splits;
+    p.out.splits = splits;
+    const int64_t ctas = units * splits * p.row_tiles;
+    if (ctas > INT_MAX) return cudaErrorInvalidConfiguration;
+    const dim3 grid((unsigned)ctas, bv.batch);
+    cudaError_t e = mv.d <= 64 ? launch<64>(ctx, maps, p, grid, stream) : launch<128>(ctx, maps, p, grid, stream);
+    if (e == cudaSuccess && splits > 1) e = launch_merge_splits(ctx, bv, p.out, stream);
+    return e;
+}
+
+}  // namespace finch

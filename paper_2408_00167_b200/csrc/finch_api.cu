@@ -11,8 +11,6 @@
 
 using namespace finch;
 
-struct finch_ctx : public Ctx {};
-
 namespace {
 
 constexpr size_t kAlign = 256;
@@ -20,7 +18,11 @@ inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
-finch_status check_tensor(const finch_ctx *ctx, const finch_tensor *t, bool allow_null_ptr) {
+}  // namespace
+
+namespace finch {
+
+finch_status check_tensor(const Ctx *ctx, const finch_tensor *t, bool allow_null_ptr) {
     if (!t) return FINCH_ERR_INVALID_ARG;
     if (!t->ptr) return allow_null_ptr ? FINCH_OK : FINCH_ERR_INVALID_ARG;
     const int64_t e = ctx->model.elem_bytes;
@@ -30,7 +32,7 @@ finch_status check_tensor(const finch_ctx *ctx, const finch_tensor *t, bool allo
     return FINCH_OK;
 }
 
-finch_status check_batch(const finch_ctx *ctx, const finch_batch *b) {
+finch_status check_batch(const Ctx *ctx, const finch_batch *b) {
     if (!ctx || !b) return FINCH_ERR_INVALID_ARG;
     if (b->batch < 0 || b->batch > ctx->cfg.max_batch) return FINCH_ERR_INVALID_ARG;
     if (b->total_q < 0 || b->total_chunk < 0 || b->total_cache < 0) return FINCH_ERR_INVALID_ARG;
@@ -44,6 +46,42 @@ finch_status check_batch(const finch_ctx *ctx, const finch_batch *b) {
         return FINCH_ERR_INVALID_ARG;
     return FINCH_OK;
 }
+
+// Do two [layers][heads][tokens][head_dim] views share a byte?  Their byte extents are compared; extents that
+// intersect are still disjoint when both views have the same strides, whole rows as their head and layer strides,
+// and base pointers that differ by a shift which keeps every row of one between the rows of the other (K and V
+// interleaved in one buffer).  Anything else that intersects, but for the layout below, counts as an overlap.
+bool views_overlap(const Ctx *ctx, const finch_tensor *a, int64_t a_tokens, int a_heads, const finch_tensor *b, int64_t b_tokens,
+                   int b_heads) {
+    if (!a || !b || !a->ptr || !b->ptr || a_tokens <= 0 || b_tokens <= 0) return false;
+    const ModelView &mv = ctx->model;
+    const int64_t e = mv.elem_bytes, row = (int64_t)mv.d * e;
+    auto extent = [&](const finch_tensor *t, int64_t tokens, int heads) {
+        return ((int64_t)(mv.L - 1) * t->stride_layer + (int64_t)(heads - 1) * t->stride_head +
+                (tokens - 1) * t->stride_tok) * e + row;
+    };
+    const uintptr_t a0 = (uintptr_t)a->ptr, b0 = (uintptr_t)b->ptr;
+    const uintptr_t a1 = a0 + (uintptr_t)extent(a, a_tokens, a_heads), b1 = b0 + (uintptr_t)extent(b, b_tokens, b_heads);
+    if (a1 <= b0 || b1 <= a0) return false;
+    const int64_t pitch = a->stride_tok * e;
+    if (a->stride_tok == b->stride_tok && a->stride_head == b->stride_head && a->stride_layer == b->stride_layer &&
+        a->stride_head % a->stride_tok == 0 && a->stride_layer % a->stride_tok == 0 && pitch >= 2 * row) {
+        const int64_t shift = (int64_t)((a0 > b0 ? a0 - b0 : b0 - a0) % (uintptr_t)pitch);
+        if (shift >= row && shift <= pitch - row) return false;  // rows of one lie in the gaps of the other
+    }
+    // .. or all heads of a token side by side, whole tokens as the layer strides, and the heads of one tensor in front of those
+    // of the other within a token (queries and keys of a fused projection)
+    const int64_t wa = ((int64_t)(a_heads - 1) * a->stride_head + mv.d) * e, wb = ((int64_t)(b_heads - 1) * b->stride_head + mv.d) * e;
+    if (a->stride_tok == b->stride_tok && wa + wb <= pitch && (mv.L == 1 || (a->stride_layer == b->stride_layer && a->stride_layer % a->stride_tok == 0))) {
+        const int64_t ahead = a0 <= b0 ? (int64_t)((b0 - a0) % (uintptr_t)pitch) : pitch - (int64_t)((a0 - b0) % (uintptr_t)pitch);
+        if (ahead >= wa && ahead <= pitch - wb) return false;
+    }
+    return true;
+}
+
+}  // namespace finch
+
+namespace {
 
 struct WsLayout {
     size_t lse_off, lse_bytes;        // scoring scratch: row statistics per key split and group, column sums per KV head
@@ -73,31 +111,6 @@ WsLayout ws_layout(const finch_ctx *ctx, const finch_batch *b) {
 }
 
 finch_status cuda_status(cudaError_t e) { return e == cudaSuccess ? FINCH_OK : FINCH_ERR_CUDA; }
-
-// Do two [layers][heads][tokens][head_dim] views share a byte?  Their byte extents are compared; extents that
-// intersect are still disjoint when both views have the same strides, whole rows as their head and layer strides,
-// and base pointers that differ by a shift which keeps every row of one between the rows of the other (K and V
-// interleaved in one buffer).  Anything else that intersects counts as an overlap.
-bool views_overlap(const finch_ctx *ctx, const finch_tensor *a, int64_t a_tokens, const finch_tensor *b,
-                   int64_t b_tokens) {
-    if (!a || !b || !a->ptr || !b->ptr || a_tokens <= 0 || b_tokens <= 0) return false;
-    const ModelView &mv = ctx->model;
-    const int64_t e = mv.elem_bytes, row = (int64_t)mv.d * e;
-    auto extent = [&](const finch_tensor *t, int64_t tokens) {
-        return ((int64_t)(mv.L - 1) * t->stride_layer + (int64_t)(mv.Hkv - 1) * t->stride_head +
-                (tokens - 1) * t->stride_tok) * e + row;
-    };
-    const uintptr_t a0 = (uintptr_t)a->ptr, b0 = (uintptr_t)b->ptr;
-    const uintptr_t a1 = a0 + (uintptr_t)extent(a, a_tokens), b1 = b0 + (uintptr_t)extent(b, b_tokens);
-    if (a1 <= b0 || b1 <= a0) return false;
-    const int64_t pitch = a->stride_tok * e;
-    if (a->stride_tok == b->stride_tok && a->stride_head == b->stride_head && a->stride_layer == b->stride_layer &&
-        a->stride_head % a->stride_tok == 0 && a->stride_layer % a->stride_tok == 0 && pitch >= 2 * row) {
-        const int64_t shift = (int64_t)((a0 > b0 ? a0 - b0 : b0 - a0) % (uintptr_t)pitch);
-        if (shift >= row && shift <= pitch - row) return false;  // rows of one lie in the gaps of the other
-    }
-    return true;
-}
 
 finch_status validate_score(const finch_ctx *ctx, const finch_tensor *q, const finch_tensor *cache_k,
                             const finch_tensor *chunk_k, const finch_batch *batch) {
@@ -133,10 +146,11 @@ finch_status validate_compact(const finch_ctx *ctx, const int32_t *kept_idx, con
     const finch_tensor *outs[2] = {out_k, out_v};
     const finch_tensor *ins[4] = {cache_k, cache_v, chunk_k, chunk_v};
     const int64_t in_tokens[4] = {batch->total_cache, batch->total_cache, batch->total_chunk, batch->total_chunk};
+    const int kv = ctx->model.Hkv;
     for (auto o : outs)
         for (int i = 0; i < 4; ++i)
-            if (views_overlap(ctx, o, batch->total_cache, ins[i], in_tokens[i])) return FINCH_ERR_INVALID_ARG;
-    if (views_overlap(ctx, out_k, batch->total_cache, out_v, batch->total_cache)) return FINCH_ERR_INVALID_ARG;
+            if (views_overlap(ctx, o, batch->total_cache, kv, ins[i], in_tokens[i], kv)) return FINCH_ERR_INVALID_ARG;
+    if (views_overlap(ctx, out_k, batch->total_cache, kv, out_v, batch->total_cache, kv)) return FINCH_ERR_INVALID_ARG;
     return FINCH_OK;
 }
 

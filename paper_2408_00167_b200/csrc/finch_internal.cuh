@@ -68,7 +68,8 @@ struct Ctx {
     cudaEvent_t ev_entry, ev_v_ready, ev_selected;
 };
 
-enum { kSmemSelect = 0, kSmemFused = 1, kSmemTc = 9 };  // bits of smem_bits; kSmemFused + variant, kSmemTc + variant
+// bits of smem_bits; kSmemFused + variant, kSmemTc + variant, ..
+enum { kSmemSelect = 0, kSmemFused = 1, kSmemTc = 9, kSmemAttendTc = 16, kSmemAttendSimt = 18, kSmemAppend = 24 };
 
 inline TensorView view_of(const finch_tensor *t) {
     return TensorView{(const char *)t->ptr, t->stride_layer, t->stride_head, t->stride_tok};
@@ -196,4 +197,13 @@ cudaError_t launch_select_compact(const Ctx &ctx, const float *scores, const Ten
                                   const int *chunk_pos, const BatchView &bv, const TensorView &out_k, const TensorView &out_v,
                                   int *out_pos, int *kept_idx, int *out_len, cudaStream_t stream);
 
+// ---- argument checks shared by the entry points (finch_api.cu)
+finch_status check_tensor(const Ctx *ctx, const finch_tensor *t, bool allow_null_ptr);
+finch_status check_batch(const Ctx *ctx, const finch_batch *b);
+// Do two views of `heads` heads share a byte?
+bool views_overlap(const Ctx *ctx, const finch_tensor *a, int64_t a_tokens, int a_heads, const finch_tensor *b, int64_t b_tokens,
+                   int b_heads);
+
 }  // namespace finch
+
+struct finch_ctx : public finch::Ctx {};
