@@ -305,7 +305,7 @@ typedef struct {
 enum { FINCH_ROPE_PLAIN = 0, FINCH_ROPE_LINEAR = 1, FINCH_ROPE_BASE = 2, FINCH_ROPE_PARTS = 3 };
 finch_status finch_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double original, double low,
                                     double high, double *inv_freq);
-/* FINCH_ERR_UNSUPPORTED: rotary_dim is no multiple of 16. */
+/* FINCH_ERR_UNSUPPORTED: rotary_dim is no multiple of 16.  FINCH_ERR_INVALID_ARG: a frequency above 2 or not a number ... */
 finch_status finch_rope_init(finch_rope *out, int32_t rotary_dim, int32_t pairing, float magnitude, const double *inv_freq);
 
 /* For every row x of q ([n_layers][n_q_heads][tokens][head_dim]) and k ([n_layers][n_kv_heads][tokens][head_dim]):

@@ -109,7 +109,7 @@ finch_status finch_rope_init(finch_rope *out, int32_t rotary_dim, int32_t pairin
     if (!isfinite(magnitude)) return FINCH_ERR_INVALID_ARG;
     if (rotary_dim % 16) return FINCH_ERR_UNSUPPORTED;
     for (int t = 0; t < rotary_dim / 2; ++t)
-        if (!isfinite(inv_freq[t])) return FINCH_ERR_INVALID_ARG;
+        if (!(fabs(inv_freq[t]) <= 2.0)) return FINCH_ERR_INVALID_ARG;  // angles of any position stay below 2^32
     memset(out, 0, sizeof(*out));
     out->rotary_dim = rotary_dim;
     out->pairing = pairing;

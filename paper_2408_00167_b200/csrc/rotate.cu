@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(kRotThreads) rotate_kernel(RotateArgs p, const
     // rows (token, head), heads innermost: kRows of them to a warp and round
     const int rows = n_tok * n_heads;
     for (int r0 = warp * kRows; r0 < rows; r0 += kRotWarps * kRows * kAhead) {
-        float x[kAhead][kRotVec];
+        Eight<T> x[kAhead];
         const T *src[kAhead];
         T *dst[kAhead];
         int tok[kAhead];
@@ -66,31 +66,35 @@ __global__ void __launch_bounds__(kRotThreads) rotate_kernel(RotateArgs p, const
                 src[a] = (const T *)in.ptr + l * in.stride_layer + hh * in.stride_head + (int64_t)(tok0 + tok[a]) * in.stride_tok;
                 dst[a] = (T *)out.ptr + l * out.stride_layer + hh * out.stride_head + (int64_t)(tok0 + tok[a]) * out.stride_tok;
             }
-#pragma unroll
-            for (int i = 0; i < kRotVec; ++i) x[a][i] = 0.f;
-            if (src[a] && live) load8(src[a] + at * kRotVec, x[a]);
+            x[a].zero();
+            if (src[a] && live) x[a].load(src[a] + at * kRotVec);
         }
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
             const T *w = (const T *)(is_q[a] ? p.q_weight : p.k_weight);
+            float y[kRotVec];
+            x[a].get(y);
             if (__any_sync(0xffffffffu, src[a] && w)) {
                 float sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < kRotVec; ++i) sum = fmaf(x[a][i], x[a][i], sum);
+                for (int i = 0; i < kRotVec; ++i) sum = fmaf(y[i], y[i], sum);
 #pragma unroll
                 for (int m = 1; m < LPR; m <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
                 if (w) {
                     const float r = rsqrtf(sum / (float)p.d + p.eps);
-                    float g[kRotVec];
                     if (live) {
-                        load8(w + (int64_t)l * p.d + at * kRotVec, g);
+                        Eight<T> g8;
+                        float g[kRotVec];
+                        g8.load(w + (int64_t)l * p.d + at * kRotVec);
+                        g8.get(g);
 #pragma unroll
-                        for (int i = 0; i < kRotVec; ++i) x[a][i] = x[a][i] * r * g[i];
+                        for (int i = 0; i < kRotVec; ++i) y[i] = y[i] * r * g[i];
                     }
                 }
             }
-            if (p.has_rope) rotate8<LPR, false>(x[a], table + tok[a] * half, at, rope.rotary_dim, rope.pairing);
-            if (src[a] && live) store8(dst[a] + at * kRotVec, x[a]);
+            if (p.has_rope) rotate8<LPR, false>(y, table + tok[a] * half, at, rope.rotary_dim, rope.pairing);
+            x[a].set(y);
+            if (src[a] && live) x[a].store(dst[a] + at * kRotVec);
         }
     }
 }
