@@ -140,7 +140,7 @@ typedef struct {
  * compute capability 10.x or the shape is not covered, FINCH_ERR_INVALID_ARG on inconsistent fields
  * (n_q_heads not a multiple of n_kv_heads, non-positive sizes, a rotary base below 1).  *out is set only on success.
  * Device memory the context owns, freed by finch_ctx_destroy: a 4-byte status word, four 4-byte counters per layer and
- * KV head, a side stream with three events
+ * KV head, two for each SM, a side stream with three events
  * (used by finch_step_host), and, with rope_theta > 0, the cosine/sine table of the re-positioning,
  * (max_candidates + 1) x head_dim/2 pairs of fp32 (2 MiB for 4096 candidates and head_dim 128), computed in double
  * precision on the host during this call. */
@@ -368,7 +368,7 @@ finch_status finch_pages_append(finch_ctx *ctx, const finch_pages *pages, const 
  * len[b] - n_q + i + 1.  Made for the last token, or the last few; every 8 rows of a KV head (its query heads times tokens)
  * read the cache once.  Pages may be shared between requests.  A page number outside [0, n_pages) sets
  * FINCH_DEV_BAD_INDEX and its tokens count as not there.  row_lse may be NULL.
- * Workspace: finch_pages_workspace_bytes, enough for every batch with no larger total_q. */
+ * Workspace: finch_pages_workspace_bytes, the same for every call of a context (and of every context of its head_dim and device). */
 finch_status finch_pages_workspace_bytes(const finch_ctx *ctx, const finch_paged_batch *batch, size_t *out);
 finch_status finch_pages_attend(finch_ctx *ctx, const finch_pages *pages, const finch_paged_batch *batch, const finch_tensor *q,
                                 const finch_tensor *out, float *row_lse, void *ws, size_t ws_bytes, void *cuda_stream);

@@ -74,9 +74,8 @@ inline size_t attend_partial_rows(const ModelView &mv, int64_t total_q, int sms,
     return a < b ? a : b;
 }
 
-// The splits of every row of a call; one of `pages` (paged cache) or the packed batch describes the requests.
+// The splits of every row of a call.
 cudaError_t launch_merge_splits(const Ctx &ctx, const BatchView &bv, const AttendOut &out, cudaStream_t stream);
-cudaError_t launch_merge_splits_paged(const Ctx &ctx, const PagesView &pg, const PagedView &bv, const AttendOut &out, cudaStream_t stream);
 
 constexpr int kAttendTcRows = 256;    // rows of a CTA, tensor-core path
 constexpr int kAttendSimtRows = 64;   // .. of the warp-level path
@@ -91,7 +90,7 @@ cudaError_t launch_attend_simt(const Ctx &ctx, const TensorView &q, const Tensor
 cudaError_t launch_pages_append(const Ctx &ctx, const PagesView &pg, const PagedView &bv, const TensorView &k, const TensorView &v,
                                 const int *pos, const finch_rope *rope, int *out_len, cudaStream_t stream);
 cudaError_t launch_pages_attend(const Ctx &ctx, const PagesView &pg, const PagedView &bv, const TensorView &q, AttendOut out,
-                                size_t partial_rows, cudaStream_t stream);
+                                cudaStream_t stream);
 cudaError_t launch_rotate(const Ctx &ctx, const TensorView &q, const TensorView &k, const TensorView &out_q, const TensorView &out_k,
                           int tokens, const int *pos, const finch_rope *rope, const void *q_weight, const void *k_weight, float eps,
                           cudaStream_t stream);

@@ -7,33 +7,22 @@ namespace {
 
 struct MergeArgs {
     ModelView mv;
-    BatchView bv;      // packed batch
-    PagesView pg;      // or paged
-    PagedView pb;
+    BatchView bv;
     AttendOut out;
-    int max_q, total_q;
 };
 
-template <typename T, bool PAGED>
+template <typename T>
 __global__ void __launch_bounds__(128) merge_kernel(MergeArgs p) {
     dependency_wait();
     const ModelView &mv = p.mv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.y;
-    int row0, n;
-    if (PAGED) {
-        const PagedInfo u = paged_info(p.pg, p.pb, b, false);
-        if (!u.ok) return;
-        row0 = u.row0, n = u.n;
-    } else {
-        const UnitInfo u = unit_info(mv, p.bv, 0, b);
-        if (!u.ok) return;
-        row0 = u.q0, n = u.n_q;
-    }
+    const UnitInfo u = unit_info(mv, p.bv, 0, b);
+    if (!u.ok) return;
     const int64_t id = (int64_t)blockIdx.x * 4 + warp;
-    if (id >= (int64_t)p.max_q * mv.L * mv.Hq) return;
-    const int i = (int)(id % p.max_q), lh = (int)(id / p.max_q), l = lh / mv.Hq, h = lh - l * mv.Hq;
-    if (i >= n) return;
-    const int64_t rows = (int64_t)mv.L * mv.Hq * p.total_q, row = attend_row(mv, p.total_q, l, h, row0 + i);
+    if (id >= (int64_t)p.bv.max_q * mv.L * mv.Hq) return;
+    const int i = (int)(id % p.bv.max_q), lh = (int)(id / p.bv.max_q), l = lh / mv.Hq, h = lh - l * mv.Hq;
+    if (i >= u.n_q) return;
+    const int64_t rows = (int64_t)mv.L * mv.Hq * p.bv.total_q, row = attend_row(mv, p.bv.total_q, l, h, u.q0 + i);
     const float2 ml = lane < p.out.splits ? p.out.part_ml[lane * rows + row] : make_float2(-INFINITY, 0.f);
     float m = ml.y == 0.f ? -INFINITY : ml.x;
 #pragma unroll
@@ -58,8 +47,8 @@ __global__ void __launch_bounds__(128) merge_kernel(MergeArgs p) {
         }
     }
     float lse;
-    const float inv = attend_finish(m, l_sum, PAGED ? nullptr : p.bv.self_lse, row, lse);
-    T *dst = (T *)p.out.ptr + l * p.out.stride_layer + h * p.out.stride_head + (int64_t)(row0 + i) * p.out.stride_tok;
+    const float inv = attend_finish(m, l_sum, p.bv.self_lse, row, lse);
+    T *dst = (T *)p.out.ptr + l * p.out.stride_layer + h * p.out.stride_head + (int64_t)(u.q0 + i) * p.out.stride_tok;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const int d = c * 128 + lane * 4;
@@ -69,22 +58,15 @@ __global__ void __launch_bounds__(128) merge_kernel(MergeArgs p) {
     if (p.out.row_lse && lane == 0) p.out.row_lse[row] = lse;
 }
 
-template <bool PAGED>
-cudaError_t launch(const Ctx &ctx, const MergeArgs &p, int batch, cudaStream_t stream) {
-    const int64_t ids = (int64_t)p.max_q * p.mv.L * p.mv.Hq;
-    ctx.launches += 1;
-    const dim3 grid((unsigned)((ids + 3) / 4), batch);
-    return ctx.model.elem_bytes == 4 ? launch_chained(merge_kernel<float, PAGED>, grid, dim3(128), 0, stream, p)
-                                     : launch_chained(merge_kernel<__nv_bfloat16, PAGED>, grid, dim3(128), 0, stream, p);
-}
-
 }  // namespace
 
 cudaError_t launch_merge_splits(const Ctx &ctx, const BatchView &bv, const AttendOut &out, cudaStream_t stream) {
-    return launch<false>(ctx, MergeArgs{ctx.model, bv, PagesView{}, PagedView{}, out, bv.max_q, bv.total_q}, bv.batch, stream);
-}
-cudaError_t launch_merge_splits_paged(const Ctx &ctx, const PagesView &pg, const PagedView &bv, const AttendOut &out, cudaStream_t stream) {
-    return launch<true>(ctx, MergeArgs{ctx.model, BatchView{}, pg, bv, out, bv.max_q, bv.total_q}, bv.batch, stream);
+    const MergeArgs p = {ctx.model, bv, out};
+    const int64_t rows = (int64_t)bv.max_q * p.mv.L * p.mv.Hq;
+    ctx.launches += 1;
+    const dim3 grid((unsigned)((rows + 3) / 4), bv.batch);
+    return ctx.model.elem_bytes == 4 ? launch_chained(merge_kernel<float>, grid, dim3(128), 0, stream, p)
+                                     : launch_chained(merge_kernel<__nv_bfloat16>, grid, dim3(128), 0, stream, p);
 }
 
 }  // namespace finch

@@ -231,6 +231,7 @@ finch_status finch_ctx_create(const finch_config *cfg, finch_ctx **out) {
     ctx->copy_stream = nullptr;
     ctx->ev_entry = ctx->ev_v_ready = ctx->ev_selected = nullptr;
     ctx->tickets = nullptr;
+    ctx->pieces = nullptr;
     ctx->smem_bits = 0;
     memset(ctx->clusters, 0, sizeof(ctx->clusters));
     memset(ctx->picks, 0, sizeof(ctx->picks));
@@ -255,13 +256,15 @@ finch_status finch_ctx_create(const finch_config *cfg, finch_ctx **out) {
                 if (dev >= 0) (void)cudaSetDevice(dev);
             }
         } restore{caller_device == cfg->device ? -1 : caller_device};
-        const size_t device_bytes = (1 + 4 * (size_t)mv.L * mv.Hkv) * sizeof(int);  // status word, scoring counters
+        // status word, scoring counters, counters of the paged cache's attention
+        const size_t device_bytes = (1 + 4 * (size_t)mv.L * mv.Hkv + pages_ctas(sms)) * sizeof(int);
         if (cudaSetDevice(cfg->device) != cudaSuccess || cudaMalloc(&ctx->d_status, device_bytes) != cudaSuccess) {
             (void)cudaGetLastError();
             delete ctx;
             return FINCH_ERR_OOM;
         }
         ctx->tickets = ctx->d_status + 1;
+        ctx->pieces = ctx->tickets + 4 * (size_t)mv.L * mv.Hkv;
         if (cudaMemset(ctx->d_status, 0, device_bytes) != cudaSuccess ||
             cudaStreamCreateWithFlags(&ctx->copy_stream, cudaStreamNonBlocking) != cudaSuccess ||
             cudaEventCreateWithFlags(&ctx->ev_entry, cudaEventDisableTiming) != cudaSuccess ||

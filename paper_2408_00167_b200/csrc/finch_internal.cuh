@@ -48,6 +48,7 @@ struct Ctx {
     bool dry;       // validation-only context: nothing is ever enqueued
     int sm_count;
     int *tickets;  // [2][units] counters, at most two units to a layer and KV head, of the one-kernel scoring: zero before and after every call
+    int *pieces;   // [pages_ctas(sm_count)] counters of the paged cache's attention: zero before and after every call
     // kernels whose shared-memory limit has been raised on this context's device (a driver call: once, not per launch)
     mutable uint32_t smem_bits;
     bool smem_ready(int bit) const { return smem_bits >> bit & 1u; }
@@ -196,6 +197,8 @@ cudaError_t launch_select_compact(const Ctx &ctx, const float *scores, const Ten
                                   const int *cache_pos, const TensorView &chunk_k, const TensorView &chunk_v,
                                   const int *chunk_pos, const BatchView &bv, const TensorView &out_k, const TensorView &out_v,
                                   int *out_pos, int *kept_idx, int *out_len, cudaStream_t stream);
+
+int pages_ctas(int sms);  // CTAs of the paged cache's attention, at most: each has two pieces of kPagesRows rows
 
 // ---- argument checks shared by the entry points (finch_api.cu)
 finch_status check_tensor(const Ctx *ctx, const finch_tensor *t, bool allow_null_ptr);

@@ -49,7 +49,14 @@ AttendWs attend_ws(const ModelView &mv, int64_t total_q, int sms, int rows_per_c
 int sm_count(const finch_ctx *ctx) { return ctx->sm_count > 0 ? ctx->sm_count : 148; }
 // rows of the CTAs that there can be splits of: the larger of the two paths' (a batch's tensors may keep it off the tensor cores)
 AttendWs attend_ws(const finch_ctx *ctx, int64_t total_q) { return attend_ws(ctx->model, total_q, sm_count(ctx), kAttendTcRows); }
-AttendWs pages_ws(const finch_ctx *ctx, int64_t total_q) { return attend_ws(ctx->model, total_q, 2 * sm_count(ctx), kPagesRows); }
+// pieces of units of the paged cache's attention
+AttendWs pages_ws(const finch_ctx *ctx) {
+    AttendWs w;
+    w.rows = (size_t)pages_ctas(sm_count(ctx)) * 2 * kPagesRows;
+    w.ml_off = align_up(w.rows * ctx->model.d * sizeof(float));
+    w.total = w.ml_off + align_up(w.rows * sizeof(float2));
+    return w;
+}
 
 AttendOut attend_out(const finch_tensor *out, float *row_lse, void *ws, const AttendWs &w) {
     AttendOut o = {(char *)out->ptr, out->stride_layer, out->stride_head, out->stride_tok, row_lse, (float *)ws, (float2 *)((char *)ws + w.ml_off), 1};
@@ -212,8 +219,8 @@ finch_status finch_pages_append(finch_ctx *ctx, const finch_pages *pages, const 
 }
 
 finch_status finch_pages_workspace_bytes(const finch_ctx *ctx, const finch_paged_batch *batch, size_t *out) {
-    if (!ctx || !batch || !out || batch->total_q < 0) return FINCH_ERR_INVALID_ARG;
-    *out = pages_ws(ctx, batch->total_q).total;
+    if (!ctx || !batch || !out || batch->batch < 0 || batch->batch > ctx->cfg.max_batch) return FINCH_ERR_INVALID_ARG;
+    *out = pages_ws(ctx).total;
     return FINCH_OK;
 }
 
@@ -227,10 +234,10 @@ finch_status finch_pages_attend(finch_ctx *ctx, const finch_pages *pages, const 
     if (views_overlap(ctx, out, batch->total_q, ctx->model.Hq, q, batch->total_q, ctx->model.Hq)) return FINCH_ERR_INVALID_ARG;
     if (!ws) return FINCH_ERR_INVALID_ARG;
     if (!aligned16(ws)) return FINCH_ERR_BAD_LAYOUT;
-    const AttendWs w = pages_ws(ctx, batch->total_q);
+    const AttendWs w = pages_ws(ctx);
     if (ws_bytes < w.total) return FINCH_ERR_WORKSPACE_TOO_SMALL;
     if ((s = check_device(ctx))) return s;
-    return cuda_status(launch_pages_attend(*ctx, view_of(pages), view_of(batch), view_of(q), attend_out(out, row_lse, ws, w), w.rows,
+    return cuda_status(launch_pages_attend(*ctx, view_of(pages), view_of(batch), view_of(q), attend_out(out, row_lse, ws, w),
                                            (cudaStream_t)cuda_stream));
 }
 

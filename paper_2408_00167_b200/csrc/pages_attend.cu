@@ -2,37 +2,141 @@
 //
 // Bound by the bytes of the cache: a page and KV head are 2 x 64 x d bytes that 8 query rows share.  A warp takes whole pages straight
 // from global memory into the registers of mma.sync fragments, 16 bytes a lane and load: which dimension is which k index is free as
-// long as both operands agree, and so is the order of the keys and, for the output, of the columns.  Codes turn into f16 exactly
-// (two at a time); of V, whose pairs along k are two keys, bytes of two rows are interleaved first.
+// long as both operands agree, and so is the order of the keys and, for the output, of the rows.  Codes turn into f16 exactly (two
+// at a time); of V, whose pairs along k are two keys, bytes of two rows are interleaved first.
 //
-//   S = Q K^T   m = 16: rows 0-7 are the f16 heads of 8 query rows, rows 8-15 what the first rounding cut off, so that
-//               q enters with 22 bits; a row is scaled by a power of two first, whatever its range.  Page and row scales
-//               multiply the logits.
-//   O += P V    the same for P = 2^(s - m) in [0, 1]; a page's product is folded into O (fp32) with its V scale.
+//   S^T = K Q^T   16 keys x 8 query rows.  Rows of Q are f16 after a power of two took their range: exact for bf16 inputs; fp32 inputs
+//                 enter as two f16 parts, 22 bits.  Page and row scales multiply the logits.
+//   O^T += V^T P^T  16 dimensions x 8 rows.  P = 2^(s - m) in [0, 1] enters as two f16 parts, turned from the layout of S^T by
+//                 movmatrix; a page's product is folded into O (fp32) with its V scale.
 //
 // (tcgen05 wants 128 rows and its operands in shared memory: 8 rows would waste 15/16 of it and every code would make a second trip
-// through shared memory.)  Keys that not all rows see and the open rows are taken one at a time with fp32 multiply-adds, dealt
-// out over all warps of the unit.  Splits of a unit are merged by merge_splits.
+// through shared memory.)  The open rows go the same way, 16 to a warp, as f16 parts scaled by a power of two.
+//
+// The work is a list of items: for every request, layer, KV head and group of 8 rows (a unit) its full pages, then one for the open
+// rows.  A CTA takes an equal share of consecutive items: all CTAs have the same number of pages, whatever the lengths.  A unit within
+// one CTA is finished there; pieces of others go to the CTA's two slots of the workspace (its first piece, its last), and the CTA that
+// delivers the last piece of a unit adds them in their order.
 #include "attend.cuh"
 
 namespace finch {
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32, kRows = kPagesRows;
+constexpr int kCtasPerSm = 2;
+constexpr int kScan = 4;   // requests of a lane and step of the search for a CTA's items
 
 struct DecodeArgs {
     ModelView mv;
     PagesView pg;
     PagedView bv;
     TensorView q;
-    AttendOut out;
+    AttendOut out;      // part_o [2 C][8][d], part_ml [2 C][8]
+    int *pieces;        // [C] pieces delivered of the unit that begins in a CTA and ends in another; zero before and after a call
     int *status;
-    int row_groups;
     float scale2;
 };
 
-__device__ __forceinline__ uint32_t half2_of(__half a, __half b) {
-    const __half2 v = __halves2half2(a, b);
+struct Request {
+    PagedInfo u;
+    int pages;   // items of a unit: full pages, one more for open rows (or for nothing at all)
+    int groups;  // of rows
+    int units;   // at most INT_MAX / 8, which the host checks of the bounds
+    __device__ __forceinline__ int items() const { return pages + (u.len % kPage > 0 || pages == 0); }
+    __device__ __forceinline__ int64_t all_items() const { return (int64_t)units * items(); }
+};
+__device__ __forceinline__ Request request_of(const DecodeArgs &p, int b) {
+    Request r;
+    r.u = paged_info(p.pg, p.bv, b, false);
+    r.u.ok = r.u.ok && r.u.len / kPage <= p.pg.table_width;
+    r.pages = r.u.ok ? r.u.len / kPage : 0;
+    r.groups = r.u.ok ? (r.u.n * p.mv.g + kRows - 1) / kRows : 0;
+    r.units = r.groups * p.mv.Hkv * p.mv.L;
+    return r;
+}
+
+// A quotient that fits an int, in 32 bits where its operands do.
+__device__ __forceinline__ int quotient(int64_t a, int64_t b) {
+    return a <= INT_MAX && b <= INT_MAX ? (int)a / (int)b : (int)(a / b);
+}
+// Equal shares: `more` CTAs have one item above `each`.
+struct Shares {
+    int64_t each;
+    int more;
+    __device__ __forceinline__ Shares(int64_t items, int ctas) {
+        each = items <= INT_MAX ? (int)items / ctas : items / ctas;
+        more = (int)(items - each * ctas);
+    }
+    __device__ __forceinline__ int64_t begin(int c) const { return each * c + min(c, more); }
+    __device__ __forceinline__ int of(int64_t item) const {
+        const int64_t big = (each + 1) * more;
+        return item < big ? quotient(item, each + 1) : more + quotient(item - big, each);
+    }
+};
+
+// Where a CTA's items begin: request, and the items in front of it.  Every warp searches by itself, kScan requests to a lane.
+struct Place {
+    int b;
+    int64_t in_front, total;
+};
+__device__ __forceinline__ Place find_items(const DecodeArgs &p) {
+    const int lane = threadIdx.x & 31, batch = p.bv.batch;
+    Place place = {0, 0, 0};
+    if (batch == 1) {
+        const Request r = request_of(p, 0);
+        if (!r.u.ok && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, FINCH_DEV_BAD_BATCH);
+        place.total = r.all_items();
+        return place;
+    }
+    const bool one_step = batch <= 32 * kScan;
+    for (int pass = one_step ? 1 : 0; pass < 2; ++pass) {
+        int64_t before = 0;
+        for (int base = 0; base < batch; base += 32 * kScan) {
+            int64_t n[kScan], mine = 0;
+#pragma unroll
+            for (int i = 0; i < kScan; ++i) {
+                const int b = base + lane * kScan + i;
+                n[i] = 0;
+                if (b < batch) {
+                    const Request r = request_of(p, b);
+                    n[i] = r.all_items();
+                    if (!r.u.ok && blockIdx.x == 0 && threadIdx.x < 32) atomicOr(p.status, FINCH_DEV_BAD_BATCH);
+                }
+                mine += n[i];
+            }
+            int64_t incl = mine;
+#pragma unroll
+            for (int x = 1; x < 32; x <<= 1) {
+                const int64_t up = __shfl_up_sync(0xffffffffu, incl, x);
+                if (lane >= x) incl += up;
+            }
+            int64_t at = before + incl - mine;
+            before += __shfl_sync(0xffffffffu, incl, 31);
+            if (one_step) place.total = before;
+            if (pass == 1) {
+                const int64_t begin = Shares(place.total, gridDim.x).begin(blockIdx.x);
+                int hit = -1;
+                int64_t hit_at = 0;
+#pragma unroll
+                for (int i = 0; i < kScan; ++i) {
+                    if (at <= begin && begin < at + n[i]) hit = base + lane * kScan + i, hit_at = at;
+                    at += n[i];
+                }
+                const unsigned who = __ballot_sync(0xffffffffu, hit >= 0);
+                if (who) {
+                    place.b = __shfl_sync(0xffffffffu, hit, __ffs(who) - 1);
+                    place.in_front = __shfl_sync(0xffffffffu, hit_at, __ffs(who) - 1);
+                    return place;
+                }
+            }
+        }
+        place.total = before;
+    }
+    return place;  // no items at all
+}
+
+__device__ __forceinline__ uint32_t half2_of(float x, float y) {
+    const __half2 v = __floats2half2_rn(x, y);
     return *(const uint32_t *)&v;
 }
 // codes in the low / high 16 bits of w -> two f16
@@ -46,20 +150,32 @@ __device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
     return r;
 }
-__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {  // an 8 x 8 matrix of f16, two of a row to a lane
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
 }
 // x, y -> their f16 heads and what is left of them, also in f16
 __device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t &lo) {
-    const __half hx = __float2half_rn(x), hy = __float2half_rn(y);
-    hi = half2_of(hx, hy);
-    lo = half2_of(__float2half_rn(x - __half2float(hx)), __float2half_rn(y - __half2float(hy)));
+    hi = half2_of(x, y);
+    const float2 h = __half22float2(*(const __half2 *)&hi);
+    lo = half2_of(x - h.x, y - h.y);
+}
+// The power of two at or below a magnitude's, and its inverse, where both are normal numbers.
+__device__ __forceinline__ void power_of_two(float top, float &up, float &down) {
+    int ex = (int)(__float_as_uint(top) >> 23) - 127;
+    ex = top > 0.f ? max(-126, min(126, ex)) : 0;
+    up = __uint_as_float((uint32_t)(127 + ex) << 23);
+    down = __uint_as_float((uint32_t)(127 - ex) << 23);
 }
 // W consecutive words, aligned to their largest power of two
 template <int W>
-__device__ __forceinline__ void load_words(uint32_t *r, const uint8_t *p) {
+__device__ __forceinline__ void load_words(uint32_t *r, const void *p) {
     if constexpr (W % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < W; i += 4) {
@@ -77,281 +193,414 @@ __device__ __forceinline__ void load_words(uint32_t *r, const uint8_t *p) {
         for (int i = 0; i < W; ++i) r[i] = __ldg((const uint32_t *)p + i);
     }
 }
+template <typename T>
+__device__ __forceinline__ void two_of(const uint32_t *w, int i, float &x, float &y) {  // elements 2i and 2i + 1 of packed words
+    if constexpr (sizeof(T) == 4)
+        x = __uint_as_float(w[2 * i]), y = __uint_as_float(w[2 * i + 1]);
+    else
+        x = __uint_as_float(w[i] << 16), y = __uint_as_float(w[i] & 0xffff0000u);
+}
 
 template <int D>
 struct Geometry {
     static constexpr int kKeys = D <= 128 ? 64 : 16;       // keys of a page that a warp holds at a time
-    static constexpr int kVec = D % 64 == 0 ? 16 : 8;      // bytes of a K row that a lane loads at a time
-    static constexpr int kChunks = D / (4 * kVec);
-    static constexpr int kSteps = D / 16;                  // k steps of S
-    static constexpr int kTiles = kKeys / 8;               // key tiles of S
-    static constexpr int kWords = D / 32;                  // words of a V row that a lane loads
+    static constexpr int kVec = D % 64 == 0 ? 16 : 8;      // neighbouring dimensions of a K or Q row in a lane
+    static constexpr int kChunks = D / (4 * kVec);         // .. and how many such runs
+    static constexpr int kSteps = D / 16;                  // k steps of S^T: four dimensions of a lane each
+    static constexpr int kTiles = kKeys / 16;              // key tiles
+    static constexpr int kWords = D / 32;                  // words of a V row's codes in a lane
+};
+
+// A warp's running result for 8 rows: lane (gid, tid) has rows 2 tid and 2 tid + 1, and of them dimensions gid D/8 .. + D/8 - 1.
+template <int D>
+struct Running {
+    float m[2], sum[2], o[D / 8][2];
+    __device__ __forceinline__ void clear() {
+        m[0] = m[1] = -INFINITY, sum[0] = sum[1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = 0.f;
+    }
+    // Softmax step over NT tiles of 16 keys: s[t] = logits of (key gid, rows 2 tid, 2 tid + 1), (key gid + 8, ..).  Leaves P in ph / pl
+    // as B fragments, and the factors of what was before in corr.
+    template <int NT>
+    __device__ __forceinline__ void weights(float (&s)[NT][4], uint32_t (&ph)[NT][2], uint32_t (&pl)[NT][2], float (&corr)[2]) {
+        float now[2] = {m[0], m[1]}, ref[2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) now[i % 2] = fmaxf(now[i % 2], s[t][i]);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) now[r] = fmaxf(now[r], __shfl_xor_sync(0xffffffffu, now[r], x));
+            ref[r] = now[r] == -INFINITY ? 0.f : now[r];
+            corr[r] = tc::ex2(m[r] - ref[r]);
+            m[r] = now[r];
+            sum[r] *= corr[r];  // a lane's own keys only: the lanes' sums are added at the end
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[t][i] = tc::ex2(s[t][i] - ref[i % 2]);
+                sum[i % 2] += s[t][i];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t hi, lo;
+                split2(s[t][2 * h], s[t][2 * h + 1], hi, lo);
+                ph[t][h] = transposed(hi), pl[t][h] = transposed(lo);
+            }
+        }
+    }
+    __device__ __forceinline__ void fold(int i, const float (&c)[4], float scale, const float (&corr)[2]) {
+        o[i][0] = fmaf(scale, c[0], o[i][0] * corr[0]), o[i][1] = fmaf(scale, c[1], o[i][1] * corr[1]);
+        o[i + 1][0] = fmaf(scale, c[2], o[i + 1][0] * corr[0]), o[i + 1][1] = fmaf(scale, c[3], o[i + 1][1] * corr[1]);
+    }
 };
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
     using Geo = Geometry<D>;
-    __shared__ __align__(16) float qs[kRows][D];
-    __shared__ __align__(16) float part[kWarps][kRows][D];
+    constexpr bool kTwoParts = sizeof(T) == 4;   // of a query row, of open rows
+    constexpr int kWordsT = sizeof(T) == 4 ? 1 : 2;  // elements to a word
+    __shared__ __align__(16) float part[kWarps][kRows][D + 4];
     __shared__ float2 part_ml[kWarps][kRows];
+    __shared__ int last_s;
     dependency_wait();
     const ModelView &mv = p.mv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tid = lane & 3;
-    const int b = blockIdx.y, l = blockIdx.z;
-    int x = blockIdx.x;
-    const int split = x % p.out.splits;
-    x /= p.out.splits;
-    const int kvh = x % mv.Hkv, rg = x / mv.Hkv;
-    const PagedInfo u = paged_info(p.pg, p.bv, b, false);
-    if (!u.ok || u.len / kPage > p.pg.table_width) {
-        if (threadIdx.x == 0) atomicOr(p.status, FINCH_DEV_BAD_BATCH);
-        return;
-    }
-    const int rows = min(kRows, u.n * mv.g - rg * kRows);  // row r of the group: token (rg * 8 + r) / g, query head (..) % g of the KV head
-    if (rows <= 0) return;
-    auto token = [&](int r) { return (rg * kRows + r) / mv.g; };
-    auto limit = [&](int r) { return max(0, u.len - u.n + token(r) + 1); };
-    const int least = limit(0), most = limit(rows - 1);
-    const int full = min(u.len, least) / kPage;            // pages that every row sees whole
+    const Place place = find_items(p);
+    const Shares shares(place.total, gridDim.x);
+    int64_t at = shares.begin(blockIdx.x);
+    const int64_t end = shares.begin(blockIdx.x + 1);
+    if (at >= end) return;
+    int b = place.b;
+    int64_t in_front = place.in_front;
+    Request req = request_of(p, b);
 
-    for (int i = threadIdx.x; i < kRows * D; i += kThreads) {
-        const int r = i / D, c = i % D;
-        float v = 0.f;
-        if (r < rows)
-            v = (float)((const T *)p.q.ptr)[l * p.q.stride_layer + (int64_t)(kvh * mv.g + (rg * kRows + r) % mv.g) * p.q.stride_head +
-                                            (int64_t)(u.row0 + token(r)) * p.q.stride_tok + c];
-        qs[r][c] = v * p.scale2;
-    }
-    __syncthreads();
-
-    const int *table = p.pg.table + (int64_t)b * p.pg.table_width;
-    const int page0 = (int)((int64_t)full * split / p.out.splits), page1 = (int)((int64_t)full * (split + 1) / p.out.splits);
-    {
-        // This lane's part of Q: row gid, dimensions chunk * 4 kVec + tid * kVec + 4 j of step (chunk, j), scaled to [1, 2).
-        uint32_t qa[Geo::kSteps][4];
-        float top = 0.f;
-        for (int c = tid; c < D; c += 4) top = fmaxf(top, fabsf(qs[gid][c]));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int ex = max(-126, min(126, (top > 0.f && top < INFINITY) ? ilogbf(top) : 0));
-        const float down = exp2f((float)-ex), up = exp2f((float)ex);
-#pragma unroll
-        for (int s = 0; s < Geo::kSteps; ++s) {
-            const int e = s * 4 / Geo::kVec * 4 * Geo::kVec + tid * Geo::kVec + s * 4 % Geo::kVec;
-            const float4 v = *(const float4 *)&qs[gid][e];
-            split2(v.x * down, v.y * down, qa[s][0], qa[s][1]);
-            split2(v.z * down, v.w * down, qa[s][2], qa[s][3]);
+    for (int piece = 0; at < end; ++piece) {
+        while (at >= in_front + req.all_items()) {  // the next request that has work
+            in_front += req.all_items();
+            req = request_of(p, ++b);
         }
-        float m = -INFINITY, sum = 0.f;
-        float o[D / 8][2];
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = 0.f;
+        const PagedInfo &u = req.u;
+        const int items = req.items(), unit = quotient(at - in_front, items);
+        const int64_t unit_at = in_front + (int64_t)unit * items;
+        const int item0 = (int)(at - unit_at), item1 = (int)min((int64_t)items, item0 + (end - at));
+        const bool whole = item0 == 0 && item1 == items;
+        at += item1 - item0;
+        const int rg = unit % req.groups, kvh = unit / req.groups % mv.Hkv, l = unit / req.groups / mv.Hkv;
+        // row r of the group: token (rg * 8 + r) / g, query head (rg * 8 + r) % g of the KV head
+        const int rows = min(kRows, u.n * mv.g - rg * kRows);
+        auto token = [&](int r) { return (rg * kRows + r) / mv.g; };
+        auto limit = [&](int r) { return r < rows ? max(0, u.len - u.n + token(r) + 1) : 0; };
+        const int least = limit(0), lim[2] = {limit(2 * tid), limit(2 * tid + 1)};
 
-        uint32_t kw[Geo::kTiles][D / 16], vw[Geo::kKeys / 16][4][Geo::kWords];
-        float k_scale = 0.f, v_scale = 0.f;
-        constexpr int kParts = kPage / Geo::kKeys;
-        const int begin = page0 * kParts, end = page1 * kParts;  // parts of pages
-        int number = 0;
-        bool bad = false;
-        auto load_k = [&](int it) {
-            number = __ldg(table + it / kParts);
-            bad = number < 0 || number >= p.pg.n_pages;
-            if (bad) number = 0;                            // a page that exists: what is read of it does not count
-            const int64_t ph = p.pg.page_head(mv, l, number, kvh);
-            const uint8_t *k = p.pg.k + ph * (kPage * D) + it % kParts * Geo::kKeys * D;
-            k_scale = __ldg(p.pg.k_scale + ph);
+        // ---- Q: row gid's dimensions of this lane, scaled into [1, 2); up[r]: what logits of rows 2 tid + r are multiplied by
+        uint32_t qh[Geo::kSteps][2], ql[kTwoParts ? Geo::kSteps : 1][2];
+        float up[2];
+        {
+            uint32_t w[D / 4 / kWordsT];
+            const T *src = (const T *)p.q.ptr + l * p.q.stride_layer + (int64_t)(kvh * mv.g + (rg * kRows + gid) % mv.g) * p.q.stride_head +
+                           (int64_t)(u.row0 + token(gid)) * p.q.stride_tok;
 #pragma unroll
-            for (int j = 0; j < Geo::kTiles; ++j)
+            for (int i = 0; i < D / 4 / kWordsT; ++i) w[i] = 0;
+            if (gid < rows) {
 #pragma unroll
                 for (int c = 0; c < Geo::kChunks; ++c)
-                    load_words<Geo::kVec / 4>(&kw[j][c * (Geo::kVec / 4)], k + (8 * j + gid) * D + c * 4 * Geo::kVec + tid * Geo::kVec);
-        };
-        auto load_v = [&](int it) {
-            const int64_t ph = p.pg.page_head(mv, l, number, kvh);
-            const uint8_t *v = p.pg.v + ph * (kPage * D) + it % kParts * Geo::kKeys * D;
-            v_scale = __ldg(p.pg.v_scale + ph);
+                    load_words<Geo::kVec / kWordsT>(&w[c * Geo::kVec / kWordsT], src + c * 4 * Geo::kVec + tid * Geo::kVec);
+            }
+            float top = 0.f, x, y;
 #pragma unroll
-            for (int kk = 0; kk < Geo::kKeys / 16; ++kk)
+            for (int i = 0; i < D / 8; ++i) {
+                two_of<T>(w, i, x, y);
+                top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            float big, down;
+            power_of_two(top, big, down);
+            big *= p.scale2;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    load_words<Geo::kWords>(vw[kk][i], v + (16 * kk + i / 2 * 8 + tid * 2 + i % 2) * D + gid * (D / 8));
-        };
-        // parts of a page go to one warp, pages around the warps
-        auto next = [&](int it) { return (it + 1) % kParts ? it + 1 : it + 1 + (kWarps - 1) * kParts; };
-        int it = begin + warp * kParts;
-        if (it < end) {
-            load_k(it);
-            load_v(it);
+            for (int i = 0; i < D / 8; ++i) {
+                two_of<T>(w, i, x, y);
+                if constexpr (kTwoParts)
+                    split2(x * down, y * down, qh[i / 2][i % 2], ql[i / 2][i % 2]);
+                else
+                    qh[i / 2][i % 2] = half2_of(x * down, y * down);
+            }
+            up[0] = __shfl_sync(0xffffffffu, big, 8 * tid);
+            up[1] = __shfl_sync(0xffffffffu, big, 8 * tid + 4);
         }
-        for (; it < end; it = next(it)) {
-            float s[Geo::kTiles][2];
-            const float f = up * k_scale, vs = v_scale;
-            const bool skip = bad;
-            if (skip && lane == 0) atomicOr(p.status, FINCH_DEV_BAD_INDEX);
+        Running<D> run;
+        run.clear();
+
+        // ---- full pages: a page to a warp, the next one's K on its way under this one's softmax, its V under the next K's
+        const int *table = p.pg.table + (int64_t)b * p.pg.table_width;
+        {
+            uint32_t kw[Geo::kTiles][2][D / 16], vw[Geo::kTiles][4][Geo::kWords];
+            float k_scale = 0.f, v_scale = 0.f;
+            constexpr int kParts = kPage / Geo::kKeys;
+            const int page1 = min(item1, req.pages) * kParts;
+            int64_t ph = 0;
+            bool bad = false;
+            auto load_k = [&](int it) {
+                int number = __ldg(table + it / kParts);
+                bad = number < 0 || number >= p.pg.n_pages;
+                if (bad) number = 0;                            // a page that exists: what is read of it does not count
+                ph = p.pg.page_head(mv, l, number, kvh);
+                const uint8_t *k = p.pg.k + ph * (kPage * D) + it % kParts * Geo::kKeys * D + gid * D + tid * Geo::kVec;
+                k_scale = __ldg(p.pg.k_scale + ph);
 #pragma unroll
-            for (int j = 0; j < Geo::kTiles; ++j) {
+                for (int t = 0; t < Geo::kTiles; ++t)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int c = 0; c < Geo::kChunks; ++c)
+                            load_words<Geo::kVec / 4>(&kw[t][h][c * (Geo::kVec / 4)], k + (16 * t + 8 * h) * D + c * 4 * Geo::kVec);
+            };
+            auto load_v = [&](int it) {
+                const uint8_t *v = p.pg.v + ph * (kPage * D) + it % kParts * Geo::kKeys * D + tid * 2 * D + gid * (D / 8);
+                v_scale = __ldg(p.pg.v_scale + ph);
+#pragma unroll
+                for (int t = 0; t < Geo::kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) load_words<Geo::kWords>(vw[t][i], v + (16 * t + i / 2 * 8 + i % 2) * D);
+            };
+            auto next = [&](int it) { return (it + 1) % kParts ? it + 1 : it + 1 + (kWarps - 1) * kParts; };
+            int it = (item0 + warp) * kParts;
+            if (it < page1) {
+                load_k(it);
+                load_v(it);
+            }
+            for (; it < page1; it = next(it)) {
+                const float f[2] = {up[0] * k_scale, up[1] * k_scale};
+                const bool skip = bad;
+                if (skip && lane == 0) atomicOr(p.status, FINCH_DEV_BAD_INDEX);
+                float s[Geo::kTiles][4];
+#pragma unroll
+                for (int t = 0; t < Geo::kTiles; ++t) {
+                    float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < Geo::kSteps; ++i) {
+                        const uint32_t a0 = codes_lo(kw[t][0][i]), a1 = codes_lo(kw[t][1][i]), a2 = codes_hi(kw[t][0][i]), a3 = codes_hi(kw[t][1][i]);
+                        mma16816(c, a0, a1, a2, a3, qh[i][0], qh[i][1]);
+                        if constexpr (kTwoParts) mma16816(c, a0, a1, a2, a3, ql[i][0], ql[i][1]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[t][i] = c[i] * f[i % 2];
+                }
+                const int j0 = it * Geo::kKeys + gid;
+                if (skip || it * Geo::kKeys + Geo::kKeys > least) {
+#pragma unroll
+                    for (int t = 0; t < Geo::kTiles; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (skip || j0 + 16 * t + i / 2 * 8 >= lim[i % 2]) s[t][i] = -INFINITY;
+                }
+                const int ahead = next(it);
+                if (ahead < page1) load_k(ahead);
+                uint32_t hi[Geo::kTiles][2], lo[Geo::kTiles][2];
+                float corr[2];
+                run.weights(s, hi, lo, corr);
+                const float vs = skip ? 0.f : v_scale;
+#pragma unroll
+                for (int w = 0; w < Geo::kWords; ++w) {
+                    float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int t = 0; t < Geo::kTiles; ++t) {
+                        const uint32_t x0 = __byte_perm(vw[t][0][w], vw[t][1][w], 0x5140), x1 = __byte_perm(vw[t][0][w], vw[t][1][w], 0x7362);
+                        const uint32_t y0 = __byte_perm(vw[t][2][w], vw[t][3][w], 0x5140), y1 = __byte_perm(vw[t][2][w], vw[t][3][w], 0x7362);
+                        const uint32_t a0 = codes_lo(x0), a1 = codes_hi(x0), a2 = codes_lo(y0), a3 = codes_hi(y0);
+                        mma16816(c0, a0, a1, a2, a3, hi[t][0], hi[t][1]);
+                        mma16816(c0, a0, a1, a2, a3, lo[t][0], lo[t][1]);
+                        const uint32_t e0 = codes_lo(x1), e1 = codes_hi(x1), e2 = codes_lo(y1), e3 = codes_hi(y1);
+                        mma16816(c1, e0, e1, e2, e3, hi[t][0], hi[t][1]);
+                        mma16816(c1, e0, e1, e2, e3, lo[t][0], lo[t][1]);
+                    }
+                    run.fold(4 * w, c0, vs, corr);
+                    run.fold(4 * w + 2, c1, vs, corr);
+                }
+                if (ahead < page1) load_v(ahead);
+            }
+        }
+
+        // ---- open rows: 16 keys to a warp
+        const int rest = item1 == items ? u.len % kPage : 0, key0 = warp * 16;
+        if (key0 < rest) {
+            const int64_t open = p.pg.open_row(mv, l, u.slot, kvh) * D;
+            float s[1][4], big, down, top = 0.f, x, y;
+            {
+                uint32_t w[2][D / 4 / kWordsT];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int key = key0 + gid + 8 * h;
+                    const T *src = (const T *)p.pg.open_k + open + key * D + tid * Geo::kVec;
+#pragma unroll
+                    for (int i = 0; i < D / 4 / kWordsT; ++i) w[h][i] = 0;
+                    if (key < rest) {
+#pragma unroll
+                        for (int c = 0; c < Geo::kChunks; ++c) load_words<Geo::kVec / kWordsT>(&w[h][c * Geo::kVec / kWordsT], src + c * 4 * Geo::kVec);
+                    }
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        two_of<T>(w[h], i, x, y);
+                        top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
+                    }
+                }
+#pragma unroll
+                for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+                power_of_two(top, big, down);
                 float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int t = 0; t < Geo::kSteps; ++t) mma16816(c, qa[t], codes_lo(kw[j][t]), codes_hi(kw[j][t]));
-                s[j][0] = (c[0] + c[2]) * f;
-                s[j][1] = (c[1] + c[3]) * f;
-            }
-            const int ahead = next(it);
-            if (ahead < end) load_k(ahead);
-            float now = m;
+                for (int i = 0; i < Geo::kSteps; ++i) {
+                    uint32_t a[4], r[4];
 #pragma unroll
-            for (int j = 0; j < Geo::kTiles; ++j) {
-                if (skip) s[j][0] = s[j][1] = -INFINITY;
-                now = fmaxf(now, fmaxf(s[j][0], s[j][1]));
-            }
-            now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 1));
-            now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 2));
-            const float ref = now == -INFINITY ? 0.f : now, corr = tc::ex2(m - ref);
-            m = now;
-            sum *= corr;
-            uint32_t pa[Geo::kTiles / 2][4];
-#pragma unroll
-            for (int j = 0; j < Geo::kTiles; ++j) {
-                const float p0 = tc::ex2(s[j][0] - ref), p1 = tc::ex2(s[j][1] - ref);
-                sum += p0 + p1;
-                split2(p0, p1, pa[j / 2][j % 2 * 2], pa[j / 2][j % 2 * 2 + 1]);
-            }
-#pragma unroll
-            for (int w = 0; w < Geo::kWords; ++w) {
-                float c[4][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.f;
-#pragma unroll
-                for (int kk = 0; kk < Geo::kKeys / 16; ++kk) {
-                    const uint32_t a0 = __byte_perm(vw[kk][0][w], vw[kk][1][w], 0x5140), a1 = __byte_perm(vw[kk][0][w], vw[kk][1][w], 0x7362);
-                    const uint32_t b0 = __byte_perm(vw[kk][2][w], vw[kk][3][w], 0x5140), b1 = __byte_perm(vw[kk][2][w], vw[kk][3][w], 0x7362);
-                    mma16816(c[0], pa[kk], codes_lo(a0), codes_lo(b0));
-                    mma16816(c[1], pa[kk], codes_hi(a0), codes_hi(b0));
-                    mma16816(c[2], pa[kk], codes_lo(a1), codes_lo(b1));
-                    mma16816(c[3], pa[kk], codes_hi(a1), codes_hi(b1));
+                    for (int h = 0; h < 4; ++h) {
+                        two_of<T>(w[h % 2], 2 * i + h / 2, x, y);
+                        split2(x * down, y * down, a[h], r[h]);
+                    }
+                    mma16816(c, a[0], a[1], a[2], a[3], qh[i][0], qh[i][1]);
+                    if constexpr (kTwoParts) {
+                        mma16816(c, a[0], a[1], a[2], a[3], ql[i][0], ql[i][1]);
+                        mma16816(c, r[0], r[1], r[2], r[3], qh[i][0], qh[i][1]);
+                    }
                 }
+                const int j0 = u.len - rest + key0 + gid;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[0][i] = j0 + i / 2 * 8 < lim[i % 2] ? c[i] * (up[i % 2] * big) : -INFINITY;
+            }
+            uint32_t hi[1][2], lo[1][2];
+            float corr[2];
+            run.weights(s, hi, lo, corr);
+            uint32_t w[4][D / 8 / kWordsT];
+            top = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = key0 + tid * 2 + i / 2 * 8 + i % 2;
+#pragma unroll
+                for (int e = 0; e < D / 8 / kWordsT; ++e) w[i][e] = 0;
+                if (key < rest) load_words<D / 8 / kWordsT>(w[i], (const T *)p.pg.open_v + open + key * D + gid * (D / 8));
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e) {
+                    two_of<T>(w[i], e, x, y);
+                    top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
+                }
+            }
+#pragma unroll
+            for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+            power_of_two(top, big, down);
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) {  // dimensions 2e and 2e + 1
+                float v[4][2];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    o[4 * w + i][0] = fmaf(vs, skip ? 0.f : c[i][0] + c[i][2], o[4 * w + i][0] * corr);
-                    o[4 * w + i][1] = fmaf(vs, skip ? 0.f : c[i][1] + c[i][3], o[4 * w + i][1] * corr);
+                    two_of<T>(w[i], e, v[i][0], v[i][1]);
+                    v[i][0] *= down, v[i][1] *= down;
                 }
+                uint32_t a[4], r[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) split2(v[h / 2 * 2][h % 2], v[h / 2 * 2 + 1][h % 2], a[h], r[h]);
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+                mma16816(c, a[0], a[1], a[2], a[3], hi[0][0], hi[0][1]);
+                mma16816(c, a[0], a[1], a[2], a[3], lo[0][0], lo[0][1]);
+                if constexpr (kTwoParts) mma16816(c, r[0], r[1], r[2], r[3], hi[0][0], hi[0][1]);
+                run.fold(2 * e, c, big, corr);
             }
-            if (ahead < end) load_v(ahead);
         }
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if (tid == 0) part_ml[warp][gid] = make_float2(m, sum);
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) part[warp][gid][(tid * 2 + c) * (D / 8) + i] = o[i][c];
-    }
-    __syncwarp();
 
-    // The rest, a key at a time: a lane has D / 32 neighbouring dimensions of each row.
-    constexpr int kPer = D / 32;
-    const int rest0 = full * kPage + split * kWarps + warp, step = p.out.splits * kWarps;
-    if (rest0 < most) {
-        float m[kRows], sum[kRows], o[kRows][kPer];
+        // ---- the warps of the CTA in their order; a thread has four dimensions of a row
+        if (piece > 0) __syncthreads();  // the last piece's results are read
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            m[r] = part_ml[warp][r].x, sum[r] = part_ml[warp][r].y;
+        for (int r = 0; r < 2; ++r) {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) o[r][i] = part[warp][r][lane * kPer + i];
+            for (int x = 4; x < 32; x <<= 1) run.sum[r] += __shfl_xor_sync(0xffffffffu, run.sum[r], x);
+            if (gid == 0) part_ml[warp][2 * tid + r] = make_float2(run.m[r], run.sum[r]);
+#pragma unroll
+            for (int i = 0; i < D / 8; i += 4)
+                *(float4 *)&part[warp][2 * tid + r][gid * (D / 8) + i] = make_float4(run.o[i][r], run.o[i + 1][r], run.o[i + 2][r], run.o[i + 3][r]);
         }
-        __syncwarp();
-        for (int j = rest0; j < most; j += step) {
-            float kx[kPer], vx[kPer];
-            const int page = j / kPage;
-            if (page < u.len / kPage) {
-                const int number = __ldg(table + page);
-                if (number < 0 || number >= p.pg.n_pages) {
-                    if (lane == 0) atomicOr(p.status, FINCH_DEV_BAD_INDEX);
-                    continue;
-                }
-                const int64_t ph = p.pg.page_head(mv, l, number, kvh), at = (ph * kPage + j % kPage) * D + lane * kPer;
-                const float ks = __ldg(p.pg.k_scale + ph), vs = __ldg(p.pg.v_scale + ph);
+        __syncthreads();
+        auto finish = [&](int r, int c, float m, float sum, float4 v) {
+            const int h = kvh * mv.g + (rg * kRows + r) % mv.g, t = u.row0 + token(r);
+            const int64_t row = attend_row(mv, p.bv.total_q, l, h, t);
+            float lse;
+            const float inv = attend_finish(m, sum, nullptr, row, lse);
+            v = sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+            store4<T>((T *)p.out.ptr + l * p.out.stride_layer + h * p.out.stride_head + (int64_t)t * p.out.stride_tok + c, v);
+            if (p.out.row_lse && c == 0) p.out.row_lse[row] = lse;
+        };
+        for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4;
+            float m = -INFINITY, sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    kx[i] = (float)((const __nv_fp8_e4m3 *)p.pg.k)[at + i] * ks;
-                    vx[i] = (float)((const __nv_fp8_e4m3 *)p.pg.v)[at + i] * vs;
-                }
+            for (int w = 0; w < kWarps; ++w)
+                if (part_ml[w][r].y != 0.f) m = fmaxf(m, part_ml[w][r].x);
+            const float ref = m == -INFINITY ? 0.f : m;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float2 ml = part_ml[w][r];
+                const float f = ml.y == 0.f ? 0.f : tc::ex2(ml.x - ref);
+                sum = fmaf(ml.y, f, sum);
+                const float4 y = *(const float4 *)&part[w][r][c];
+                v.x = fmaf(y.x, f, v.x), v.y = fmaf(y.y, f, v.y), v.z = fmaf(y.z, f, v.z), v.w = fmaf(y.w, f, v.w);
+            }
+            if (whole) {
+                finish(r, c, m, sum, v);
             } else {
-                const int64_t at = (p.pg.open_row(mv, l, u.slot, kvh) + j % kPage) * D + lane * kPer;
+                const int64_t slot = (2 * (int64_t)blockIdx.x + (piece > 0)) * kRows + r;
+                __stcg((float4 *)(p.out.part_o + slot * D + c), v);
+                if (c == 0) __stcg(p.out.part_ml + slot, make_float2(m, sum));
+            }
+        }
+        if (whole) continue;
+        // ---- the CTA that delivers a unit's last piece adds them
+        const int c0 = shares.of(unit_at), c1 = shares.of(unit_at + items - 1);
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const int n = atomicAdd(p.pieces + c0, 1);
+            last_s = n == c1 - c0;
+            if (last_s) p.pieces[c0] = 0;  // nobody else comes
+        }
+        __syncthreads();
+        if (!last_s) continue;
+        __threadfence();
+        for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4;
+            auto slot_of = [&](int cta) { return (2 * (int64_t)cta + (shares.begin(cta) < unit_at)) * kRows + r; };
+            float m = -INFINITY, sum = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            constexpr int kBatch = 8;   // pieces in flight
+            for (int base = c0; base <= c1; base += kBatch) {
+                float2 ml[kBatch];
+                float4 y[kBatch];
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    kx[i] = (float)((const T *)p.pg.open_k)[at + i];
-                    vx[i] = (float)((const T *)p.pg.open_v)[at + i];
+                for (int k = 0; k < kBatch; ++k) {
+                    const int64_t slot = slot_of(min(base + k, c1));
+                    ml[k] = __ldcg(p.out.part_ml + slot);
+                    y[k] = __ldcg((const float4 *)(p.out.part_o + slot * D + c));
+                    if (base + k > c1) ml[k].y = 0.f;
+                }
+                float now = m;
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k)
+                    if (ml[k].y != 0.f) now = fmaxf(now, ml[k].x);
+                const float ref = now == -INFINITY ? 0.f : now, corr = tc::ex2(m - ref);
+                m = now;
+                sum *= corr, v.x *= corr, v.y *= corr, v.z *= corr, v.w *= corr;
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    if (ml[k].y == 0.f) continue;  // saw none of the row's keys
+                    const float f = tc::ex2(ml[k].x - ref);
+                    sum = fmaf(ml[k].y, f, sum);
+                    v.x = fmaf(y[k].x, f, v.x), v.y = fmaf(y[k].y, f, v.y), v.z = fmaf(y[k].z, f, v.z), v.w = fmaf(y[k].w, f, v.w);
                 }
             }
-            float s[kRows];
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                s[r] = 0.f;
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) s[r] = fmaf(qs[r][lane * kPer + i], kx[i], s[r]);
-            }
-#pragma unroll
-            for (int r = 0; r < kRows; ++r)
-#pragma unroll
-                for (int w = 16; w; w >>= 1) s[r] += __shfl_xor_sync(0xffffffffu, s[r], w);
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                if (r >= rows || j >= limit(r)) continue;
-                if (s[r] > m[r]) {
-                    const float corr = tc::ex2(m[r] - s[r]);
-                    sum[r] *= corr;
-#pragma unroll
-                    for (int i = 0; i < kPer; ++i) o[r][i] *= corr;
-                    m[r] = s[r];
-                }
-                const float w = tc::ex2(s[r] - (m[r] == -INFINITY ? 0.f : m[r]));
-                sum[r] += w;
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) o[r][i] = fmaf(w, vx[i], o[r][i]);
-            }
+            finish(r, c, m, sum, v);
         }
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            if (lane == 0) part_ml[warp][r] = make_float2(m[r], sum[r]);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) part[warp][r][lane * kPer + i] = o[r][i];
-        }
-    }
-    __syncthreads();
-
-    // The warps of the CTA in their order; a thread has four dimensions of a row.
-    for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
-        const int r = i / (D / 4), c = i % (D / 4) * 4;
-        float m = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w)
-            if (part_ml[w][r].y != 0.f) m = fmaxf(m, part_ml[w][r].x);
-        const float ref = m == -INFINITY ? 0.f : m;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float2 ml = part_ml[w][r];
-            if (ml.y == 0.f) continue;
-            const float f = exp2f(ml.x - ref);
-            sum = fmaf(ml.y, f, sum);
-            const float4 y = *(const float4 *)&part[w][r][c];
-            v.x = fmaf(y.x, f, v.x), v.y = fmaf(y.y, f, v.y), v.z = fmaf(y.z, f, v.z), v.w = fmaf(y.w, f, v.w);
-        }
-        const int h = kvh * mv.g + (rg * kRows + r) % mv.g, t = u.row0 + token(r);
-        const int64_t row = attend_row(mv, p.bv.total_q, l, h, t);
-        if (p.out.splits > 1) {
-            const int64_t slot = split * ((int64_t)mv.L * mv.Hq * p.bv.total_q) + row;
-            *(float4 *)(p.out.part_o + slot * D + c) = v;
-            if (c == 0) p.out.part_ml[slot] = make_float2(m, sum);
-            continue;
-        }
-        float lse;
-        const float inv = attend_finish(m, sum, nullptr, row, lse);
-        if (sum == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
-        else v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-        store4<T>((T *)p.out.ptr + l * p.out.stride_layer + h * p.out.stride_head + (int64_t)t * p.out.stride_tok + c, v);
-        if (p.out.row_lse && c == 0) p.out.row_lse[row] = lse;
     }
 }
 
@@ -373,23 +622,20 @@ cudaError_t launch_t(const Ctx &ctx, const DecodeArgs &p, dim3 grid, cudaStream_
 
 }  // namespace
 
+int pages_ctas(int sms) { return kCtasPerSm * sms; }
+
 cudaError_t launch_pages_attend(const Ctx &ctx, const PagesView &pg, const PagedView &bv, const TensorView &q, AttendOut out,
-                                size_t partial_rows, cudaStream_t stream) {
+                                cudaStream_t stream) {
     if (bv.batch == 0 || bv.max_q == 0) return cudaSuccess;
     const ModelView &mv = ctx.model;
-    DecodeArgs p = {mv, pg, bv, q, out, ctx.d_status, (bv.max_q * mv.g + kRows - 1) / kRows, mv.scale * kLog2e};
-    const int64_t units = (int64_t)mv.L * mv.Hkv * p.row_groups * bv.batch;
-    const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
-    int splits = attend_splits(units, 2 * ctx.sm_count, bv.max_len / kPage, kWarps);
-    while (splits > 1 && splits * rows > partial_rows) --splits;
-    p.out.splits = splits;
-    cudaError_t e;
-    const int64_t ctas = (int64_t)splits * mv.Hkv * p.row_groups;
-    if (ctas > INT_MAX) return cudaErrorInvalidConfiguration;
-    const dim3 grid((unsigned)ctas, bv.batch, mv.L);
-    e = mv.elem_bytes == 4 ? launch_t<float>(ctx, p, grid, stream) : launch_t<__nv_bfloat16>(ctx, p, grid, stream);
-    if (e == cudaSuccess && splits > 1) e = launch_merge_splits_paged(ctx, pg, bv, p.out, stream);
-    return e;
+    const DecodeArgs p = {mv, pg, bv, q, out, ctx.pieces, ctx.d_status, mv.scale * kLog2e};
+    const int64_t max_units = (int64_t)mv.L * mv.Hkv * ((bv.max_q * (int64_t)mv.g + kRows - 1) / kRows);
+    if (max_units * kRows > INT_MAX) return cudaErrorInvalidConfiguration;
+    // every warp of a CTA a page where there are few
+    const int64_t items = max_units * bv.batch * (bv.max_len / kPage + 1);
+    int ctas = pages_ctas(ctx.sm_count);
+    if (items < (int64_t)ctas * kWarps) ctas = (int)((items + kWarps - 1) / kWarps);
+    return mv.elem_bytes == 4 ? launch_t<float>(ctx, p, dim3(ctas), stream) : launch_t<__nv_bfloat16>(ctx, p, dim3(ctas), stream);
 }
 
 }  // namespace finch
