@@ -70,7 +70,7 @@ struct Ctx {
 };
 
 // bits of smem_bits; kSmemFused + variant, kSmemTc + variant, ..
-enum { kSmemSelect = 0, kSmemFused = 1, kSmemTc = 9, kSmemAttendTc = 16, kSmemAttendSimt = 18, kSmemAppend = 24 };
+enum { kSmemSelect = 0, kSmemFused = 1, kSmemTc = 9, kSmemAttendTc = 16, kSmemAttendSimt = 18, kSmemAppend = 24, kSmemDecode = 26 };
 
 inline TensorView view_of(const finch_tensor *t) {
     return TensorView{(const char *)t->ptr, t->stride_layer, t->stride_head, t->stride_tok};

@@ -11,7 +11,7 @@
 //                 movmatrix; a page's product is folded into O (fp32) with its V scale.
 //
 // (tcgen05 wants 128 rows and its operands in shared memory: 8 rows would waste 15/16 of it and every code would make a second trip
-// through shared memory.)  The open rows go the same way, 16 to a warp, as f16 parts scaled by a power of two.
+// through shared memory.)  The open rows go the same way, 16 to a warp: bf16 as they are, fp32 as f16 parts scaled by a power of two.
 //
 // The work is a list of items: for every request, layer, KV head and group of 8 rows (a unit) its full pages, then one for the open
 // rows.  A CTA takes an equal share of consecutive items: all CTAs have the same number of pages, whatever the lengths.  A unit within
@@ -151,7 +151,7 @@ __device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
     return r;
 }
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -203,13 +203,43 @@ __device__ __forceinline__ void two_of(const uint32_t *w, int i, float &x, float
 
 template <int D>
 struct Geometry {
-    static constexpr int kKeys = D <= 128 ? 64 : 16;       // keys of a page that a warp holds at a time
     static constexpr int kVec = D % 64 == 0 ? 16 : 8;      // neighbouring dimensions of a K or Q row in a lane
     static constexpr int kChunks = D / (4 * kVec);         // .. and how many such runs
     static constexpr int kSteps = D / 16;                  // k steps of S^T: four dimensions of a lane each
-    static constexpr int kTiles = kKeys / 16;              // key tiles
+    static constexpr int kTiles = kPage / 16;              // key tiles
     static constexpr int kWords = D / 32;                  // words of a V row's codes in a lane
+    static constexpr int kSlot = kPage * D;                // bytes of a page's K or V of one head
+    static constexpr int kSlots = 3;                       // of a warp
+    static constexpr int kSmem = kWarps * kSlots * kSlot;
+    static_assert(kRows * (D + 4) * 4 <= kSlots * kSlot, "a warp's result takes the place of its pages");
+    // Where byte `x` of row `row` lies in a slot.  A quarter of a warp reads two rows' halves (K) or four rows' neighbouring
+    // 16 bytes (V): of rows of 128 bytes or a multiple the 16-byte pieces change places so that these are in different banks.
+    __device__ __forceinline__ static int place(int row, int x) {
+        if constexpr (D % 128 == 0) return row * D + (x ^ ((((row >> 2) ^ row) & 1) << 6 | ((row >> 1) & 1) << 5));
+        return row * D + x;
+    }
 };
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <int W>
+__device__ __forceinline__ void read_words(uint32_t *r, uint32_t addr) {
+    if constexpr (W % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < W; i += 4)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]) : "r"(addr + i * 4));
+    } else if constexpr (W % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < W; i += 2) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r[i]), "=r"(r[i + 1]) : "r"(addr + i * 4));
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[i]) : "r"(addr + i * 4));
+    }
+}
 
 // A warp's running result for 8 rows: lane (gid, tid) has rows 2 tid and 2 tid + 1, and of them dimensions gid D/8 .. + D/8 - 1.
 template <int D>
@@ -220,10 +250,10 @@ struct Running {
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = 0.f;
     }
-    // Softmax step over NT tiles of 16 keys: s[t] = logits of (key gid, rows 2 tid, 2 tid + 1), (key gid + 8, ..).  Leaves P in ph / pl
-    // as B fragments, and the factors of what was before in corr.
+    // Softmax step over NT tiles of 16 keys: s[t] = logits of (key gid, rows 2 tid, 2 tid + 1), (key gid + 8, ..) become P; corr: the
+    // factors of what was before.
     template <int NT>
-    __device__ __forceinline__ void weights(float (&s)[NT][4], uint32_t (&ph)[NT][2], uint32_t (&pl)[NT][2], float (&corr)[2]) {
+    __device__ __forceinline__ void weights(float (&s)[NT][4], float (&corr)[2]) {
         float now[2] = {m[0], m[1]}, ref[2];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -245,13 +275,19 @@ struct Running {
                 s[t][i] = tc::ex2(s[t][i] - ref[i % 2]);
                 sum[i % 2] += s[t][i];
             }
+        }
+    }
+    // P as B fragments of two f16 parts
+    template <int NT>
+    __device__ __forceinline__ static void parts(const float (&s)[NT][4], uint32_t (&ph)[NT][2], uint32_t (&pl)[NT][2]) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t hi, lo;
                 split2(s[t][2 * h], s[t][2 * h + 1], hi, lo);
                 ph[t][h] = transposed(hi), pl[t][h] = transposed(lo);
             }
-        }
     }
     __device__ __forceinline__ void fold(int i, const float (&c)[4], float scale, const float (&corr)[2]) {
         o[i][0] = fmaf(scale, c[0], o[i][0] * corr[0]), o[i][1] = fmaf(scale, c[1], o[i][1] * corr[1]);
@@ -259,17 +295,76 @@ struct Running {
     }
 };
 
+__device__ __forceinline__ void mma16816_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16 open rows of bf16, as they are: K and Q multiply exactly, P enters as three bf16 parts, 24 bits.  Keys key0 + gid (+ 8) of the
+// slot, `rest` of which hold tokens; j0 the token of key0 + gid.
+template <int D>
+__device__ __forceinline__ void open_rows_bf16(Running<D> &run, const __nv_bfloat16 *q, bool live, const __nv_bfloat16 *k, const __nv_bfloat16 *v,
+                                               int key0, int rest, int j0, const int (&lim)[2], float scale2) {
+    const int lane = threadIdx.x & 31, gid = lane >> 2, tid = lane & 3;
+    const uint2 none = make_uint2(0, 0);
+    const int ka = key0 + gid, kb = ka + 8;
+    float s[1][4] = {{0.f, 0.f, 0.f, 0.f}}, corr[2];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {  // four dimensions of the lane: 16 i + 4 tid
+        const int e = 16 * i + 4 * tid;
+        const uint2 x = ka < rest ? __ldg((const uint2 *)(k + ka * D + e)) : none, y = kb < rest ? __ldg((const uint2 *)(k + kb * D + e)) : none;
+        const uint2 z = live ? __ldg((const uint2 *)(q + e)) : none;
+        mma16816_bf16(s[0], x.x, y.x, x.y, y.y, z.x, z.y);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[0][i] = j0 + i / 2 * 8 < lim[i % 2] ? s[0][i] * scale2 : -INFINITY;
+    run.weights(s, corr);
+    uint32_t pf[3][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float x = s[0][2 * h], y = s[0][2 * h + 1];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+            const __nv_bfloat162 w = __floats2bfloat162_rn(x, y);
+            const uint32_t bits = *(const uint32_t *)&w;
+            x -= __uint_as_float(bits << 16), y -= __uint_as_float(bits & 0xffff0000u);
+            pf[n][h] = transposed(bits);
+        }
+    }
+    constexpr int kW = D / 16;  // words of a lane's D / 8 dimensions
+    uint32_t w[4][kW];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int key = key0 + tid * 2 + i / 2 * 8 + i % 2;
+#pragma unroll
+        for (int e = 0; e < kW; ++e) w[i][e] = 0;
+        if (key < rest) load_words<kW>(w[i], v + key * D + gid * (D / 8));
+    }
+#pragma unroll
+    for (int e = 0; e < kW; ++e) {
+        const uint32_t a0 = __byte_perm(w[0][e], w[1][e], 0x5410), a1 = __byte_perm(w[0][e], w[1][e], 0x7632);
+        const uint32_t a2 = __byte_perm(w[2][e], w[3][e], 0x5410), a3 = __byte_perm(w[2][e], w[3][e], 0x7632);
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < 3; ++n) mma16816_bf16(c, a0, a1, a2, a3, pf[n][0], pf[n][1]);
+        run.fold(2 * e, c, 1.f, corr);
+    }
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
     using Geo = Geometry<D>;
     constexpr bool kTwoParts = sizeof(T) == 4;   // of a query row, of open rows
     constexpr int kWordsT = sizeof(T) == 4 ? 1 : 2;  // elements to a word
-    __shared__ __align__(16) float part[kWarps][kRows][D + 4];
+    extern __shared__ __align__(128) uint8_t ring[];  // [warp][slot] pages; a warp's result [row][D + 4] in place of its pages
     __shared__ float2 part_ml[kWarps][kRows];
     __shared__ int last_s;
     dependency_wait();
     const ModelView &mv = p.mv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tid = lane & 3;
+    uint8_t *mine = ring + warp * Geo::kSlots * Geo::kSlot;
+    auto part = [&](int w, int r) { return (float *)(ring + w * Geo::kSlots * Geo::kSlot) + r * (D + 4); };
     const Place place = find_items(p);
     const Shares shares(place.total, gridDim.x);
     int64_t at = shares.begin(blockIdx.x);
@@ -296,6 +391,8 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
         auto token = [&](int r) { return (rg * kRows + r) / mv.g; };
         auto limit = [&](int r) { return r < rows ? max(0, u.len - u.n + token(r) + 1) : 0; };
         const int least = limit(0), lim[2] = {limit(2 * tid), limit(2 * tid + 1)};
+
+        if (piece > 0) __syncthreads();  // the last piece's results are read: pages may take their place
 
         // ---- Q: row gid's dimensions of this lane, scaled into [1, 2); up[r]: what logits of rows 2 tid + r are multiplied by
         uint32_t qh[Geo::kSteps][2], ql[kTwoParts ? Geo::kSteps : 1][2];
@@ -336,100 +433,141 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
         Running<D> run;
         run.clear();
 
-        // ---- full pages: a page to a warp, the next one's K on its way under this one's softmax, its V under the next K's
+        // ---- full pages: a page to a warp.  Its three slots take K and V of its pages in turn: one is read, two are on their way.
         const int *table = p.pg.table + (int64_t)b * p.pg.table_width;
         {
-            uint32_t kw[Geo::kTiles][2][D / 16], vw[Geo::kTiles][4][Geo::kWords];
+            const int page1 = min(item1, req.pages), n_mine = max(0, (page1 - (item0 + warp) + kWarps - 1) / kWarps);
+            const uint32_t mine_u = ptx::smem_u32(mine);
+            auto number_of = [&](int n) { return n < n_mine ? __ldg(table + item0 + warp + n * kWarps) : 0; };
+            auto good = [&](int number) { return number >= 0 && number < p.pg.n_pages; };
+            auto place_of = [&](int number) { return p.pg.page_head(mv, l, good(number) ? number : 0, kvh); };  // what is read of a bad one does not count
+            auto fetch = [&](int n, int number, bool is_v) {   // K or V of this warp's n-th page
+                if (n < n_mine) {
+                    const uint8_t *src = (is_v ? p.pg.v : p.pg.k) + place_of(number) * Geo::kSlot;
+                    const uint32_t slot = mine_u + (2 * n + is_v) % Geo::kSlots * Geo::kSlot;
+#pragma unroll
+                    for (int i = 0; i < Geo::kSlot / 512; ++i) {
+                        const int x = (i * 32 + lane) * 16;
+                        copy16(slot + Geo::place(x / D, x % D), src + x);
+                    }
+                }
+                copies_commit();
+            };
+            int n0 = number_of(0), n1 = number_of(1), n2 = number_of(2);
             float k_scale = 0.f, v_scale = 0.f;
-            constexpr int kParts = kPage / Geo::kKeys;
-            const int page1 = min(item1, req.pages) * kParts;
-            int64_t ph = 0;
-            bool bad = false;
-            auto load_k = [&](int it) {
-                int number = __ldg(table + it / kParts);
-                bad = number < 0 || number >= p.pg.n_pages;
-                if (bad) number = 0;                            // a page that exists: what is read of it does not count
-                ph = p.pg.page_head(mv, l, number, kvh);
-                const uint8_t *k = p.pg.k + ph * (kPage * D) + it % kParts * Geo::kKeys * D + gid * D + tid * Geo::kVec;
-                k_scale = __ldg(p.pg.k_scale + ph);
-#pragma unroll
-                for (int t = 0; t < Geo::kTiles; ++t)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int c = 0; c < Geo::kChunks; ++c)
-                            load_words<Geo::kVec / 4>(&kw[t][h][c * (Geo::kVec / 4)], k + (16 * t + 8 * h) * D + c * 4 * Geo::kVec);
-            };
-            auto load_v = [&](int it) {
-                const uint8_t *v = p.pg.v + ph * (kPage * D) + it % kParts * Geo::kKeys * D + tid * 2 * D + gid * (D / 8);
-                v_scale = __ldg(p.pg.v_scale + ph);
-#pragma unroll
-                for (int t = 0; t < Geo::kTiles; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) load_words<Geo::kWords>(vw[t][i], v + (16 * t + i / 2 * 8 + i % 2) * D);
-            };
-            auto next = [&](int it) { return (it + 1) % kParts ? it + 1 : it + 1 + (kWarps - 1) * kParts; };
-            int it = (item0 + warp) * kParts;
-            if (it < page1) {
-                load_k(it);
-                load_v(it);
-            }
-            for (; it < page1; it = next(it)) {
+            if (n_mine > 0) k_scale = __ldg(p.pg.k_scale + place_of(n0)), v_scale = __ldg(p.pg.v_scale + place_of(n0));
+            fetch(0, n0, false);
+            fetch(0, n0, true);
+            fetch(1, n1, false);
+#pragma unroll 1
+            for (int n = 0; n < n_mine; ++n) {
                 const float f[2] = {up[0] * k_scale, up[1] * k_scale};
-                const bool skip = bad;
+                const bool skip = !good(n0);
+                const float vs = skip ? 0.f : v_scale;
                 if (skip && lane == 0) atomicOr(p.status, FINCH_DEV_BAD_INDEX);
+                if (n + 1 < n_mine) k_scale = __ldg(p.pg.k_scale + place_of(n1)), v_scale = __ldg(p.pg.v_scale + place_of(n1));
+                copies_wait<2>();
+                __syncwarp();
                 float s[Geo::kTiles][4];
 #pragma unroll
-                for (int t = 0; t < Geo::kTiles; ++t) {
-                    float c[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < Geo::kTiles; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+                {
+                    const uint32_t slot = mine_u + 2 * n % Geo::kSlots * Geo::kSlot;
+                    constexpr int kW = Geo::kVec / 4;
 #pragma unroll
-                    for (int i = 0; i < Geo::kSteps; ++i) {
-                        const uint32_t a0 = codes_lo(kw[t][0][i]), a1 = codes_lo(kw[t][1][i]), a2 = codes_hi(kw[t][0][i]), a3 = codes_hi(kw[t][1][i]);
-                        mma16816(c, a0, a1, a2, a3, qh[i][0], qh[i][1]);
-                        if constexpr (kTwoParts) mma16816(c, a0, a1, a2, a3, ql[i][0], ql[i][1]);
+                    for (int c = 0; c < Geo::kChunks; ++c) {
+                        uint32_t kw[Geo::kTiles][2][kW];
+#pragma unroll
+                        for (int t = 0; t < Geo::kTiles; ++t)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                read_words<kW>(kw[t][h], slot + Geo::place(16 * t + 8 * h + gid, c * 4 * Geo::kVec + tid * Geo::kVec));
+                        // a product waits for the one before it on the same accumulator: the tiles take turns
+#pragma unroll
+                        for (int j = 0; j < kW; ++j)
+#pragma unroll
+                            for (int t = 0; t < Geo::kTiles; ++t) {
+                                const int i = c * kW + j;
+                                const uint32_t a0 = codes_lo(kw[t][0][j]), a1 = codes_lo(kw[t][1][j]), a2 = codes_hi(kw[t][0][j]), a3 = codes_hi(kw[t][1][j]);
+                                mma16816(s[t], a0, a1, a2, a3, qh[i][0], qh[i][1]);
+                                if constexpr (kTwoParts) mma16816(s[t], a0, a1, a2, a3, ql[i][0], ql[i][1]);
+                            }
                     }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[t][i] = c[i] * f[i % 2];
                 }
-                const int j0 = it * Geo::kKeys + gid;
-                if (skip || it * Geo::kKeys + Geo::kKeys > least) {
+                __syncwarp();
+                fetch(n + 1, n1, true);
+                const int j0 = (item0 + warp + n * kWarps) * kPage + gid;
+#pragma unroll
+                for (int t = 0; t < Geo::kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[t][i] *= f[i % 2];
+                if (skip || j0 - gid + kPage > least) {
 #pragma unroll
                     for (int t = 0; t < Geo::kTiles; ++t)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             if (skip || j0 + 16 * t + i / 2 * 8 >= lim[i % 2]) s[t][i] = -INFINITY;
                 }
-                const int ahead = next(it);
-                if (ahead < page1) load_k(ahead);
                 uint32_t hi[Geo::kTiles][2], lo[Geo::kTiles][2];
                 float corr[2];
-                run.weights(s, hi, lo, corr);
-                const float vs = skip ? 0.f : v_scale;
+                run.weights(s, corr);
+                run.parts(s, hi, lo);
+                copies_wait<2>();
+                __syncwarp();
+                {
+                    const uint32_t slot = mine_u + (2 * n + 1) % Geo::kSlots * Geo::kSlot;
+                    constexpr int kW = Geo::kWords, kHalf = kW > 4 ? kW / 2 : kW;   // words at a time (accumulators: 8 registers a word)
+                    static_assert(kW % kHalf == 0 || kW == 5 || kW == 7, "");
+                    constexpr int kStep = kW == 5 || kW == 7 ? kW : kHalf;
 #pragma unroll
-                for (int w = 0; w < Geo::kWords; ++w) {
-                    float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int w0 = 0; w0 < kW; w0 += kStep) {
+                        float c[2 * kStep][4];
 #pragma unroll
-                    for (int t = 0; t < Geo::kTiles; ++t) {
-                        const uint32_t x0 = __byte_perm(vw[t][0][w], vw[t][1][w], 0x5140), x1 = __byte_perm(vw[t][0][w], vw[t][1][w], 0x7362);
-                        const uint32_t y0 = __byte_perm(vw[t][2][w], vw[t][3][w], 0x5140), y1 = __byte_perm(vw[t][2][w], vw[t][3][w], 0x7362);
-                        const uint32_t a0 = codes_lo(x0), a1 = codes_hi(x0), a2 = codes_lo(y0), a3 = codes_hi(y0);
-                        mma16816(c0, a0, a1, a2, a3, hi[t][0], hi[t][1]);
-                        mma16816(c0, a0, a1, a2, a3, lo[t][0], lo[t][1]);
-                        const uint32_t e0 = codes_lo(x1), e1 = codes_hi(x1), e2 = codes_lo(y1), e3 = codes_hi(y1);
-                        mma16816(c1, e0, e1, e2, e3, hi[t][0], hi[t][1]);
-                        mma16816(c1, e0, e1, e2, e3, lo[t][0], lo[t][1]);
+                        for (int i = 0; i < 2 * kStep; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.f;
+#pragma unroll
+                        for (int t = 0; t < Geo::kTiles; ++t) {
+                            uint32_t vw[4][kStep];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                read_words<kStep>(vw[i], slot + Geo::place(16 * t + i / 2 * 8 + tid * 2 + i % 2, gid * (D / 8) + w0 * 4));
+#pragma unroll
+                            for (int w = 0; w < kStep; ++w) {
+                                const uint32_t x0 = __byte_perm(vw[0][w], vw[1][w], 0x5140), x1 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
+                                const uint32_t y0 = __byte_perm(vw[2][w], vw[3][w], 0x5140), y1 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
+                                const uint32_t a0 = codes_lo(x0), a1 = codes_hi(x0), a2 = codes_lo(y0), a3 = codes_hi(y0);
+                                const uint32_t e0 = codes_lo(x1), e1 = codes_hi(x1), e2 = codes_lo(y1), e3 = codes_hi(y1);
+                                mma16816(c[2 * w], a0, a1, a2, a3, hi[t][0], hi[t][1]);
+                                mma16816(c[2 * w + 1], e0, e1, e2, e3, hi[t][0], hi[t][1]);
+                                mma16816(c[2 * w], a0, a1, a2, a3, lo[t][0], lo[t][1]);
+                                mma16816(c[2 * w + 1], e0, e1, e2, e3, lo[t][0], lo[t][1]);
+                            }
+                        }
+#pragma unroll
+                        for (int w = 0; w < kStep; ++w) {
+                            run.fold(4 * (w0 + w), c[2 * w], vs, corr);
+                            run.fold(4 * (w0 + w) + 2, c[2 * w + 1], vs, corr);
+                        }
                     }
-                    run.fold(4 * w, c0, vs, corr);
-                    run.fold(4 * w + 2, c1, vs, corr);
                 }
-                if (ahead < page1) load_v(ahead);
+                __syncwarp();
+                n0 = n1, n1 = n2, n2 = number_of(n + 3);
+                fetch(n + 2, n1, false);
             }
+            copies_wait<0>();  // empty groups
+            __syncwarp();
         }
 
         // ---- open rows: 16 keys to a warp
         const int rest = item1 == items ? u.len % kPage : 0, key0 = warp * 16;
         if (key0 < rest) {
             const int64_t open = p.pg.open_row(mv, l, u.slot, kvh) * D;
+            const int j0 = u.len - rest + key0 + gid;
+            if constexpr (!kTwoParts) {
+                open_rows_bf16<D>(run, (const __nv_bfloat16 *)p.q.ptr + l * p.q.stride_layer + (int64_t)(kvh * mv.g + (rg * kRows + gid) % mv.g) * p.q.stride_head +
+                                           (int64_t)(u.row0 + token(gid)) * p.q.stride_tok,
+                                  gid < rows, (const __nv_bfloat16 *)p.pg.open_k + open, (const __nv_bfloat16 *)p.pg.open_v + open, key0, rest, j0, lim,
+                                  p.scale2);
+            } else {
             float s[1][4], big, down, top = 0.f, x, y;
             {
                 uint32_t w[2][D / 4 / kWordsT];
@@ -467,13 +605,13 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
                         mma16816(c, r[0], r[1], r[2], r[3], qh[i][0], qh[i][1]);
                     }
                 }
-                const int j0 = u.len - rest + key0 + gid;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[0][i] = j0 + i / 2 * 8 < lim[i % 2] ? c[i] * (up[i % 2] * big) : -INFINITY;
             }
             uint32_t hi[1][2], lo[1][2];
             float corr[2];
-            run.weights(s, hi, lo, corr);
+            run.weights(s, corr);
+            run.parts(s, hi, lo);
             uint32_t w[4][D / 8 / kWordsT];
             top = 0.f;
 #pragma unroll
@@ -508,10 +646,10 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
                 if constexpr (kTwoParts) mma16816(c, r[0], r[1], r[2], r[3], hi[0][0], hi[0][1]);
                 run.fold(2 * e, c, big, corr);
             }
+            }
         }
 
         // ---- the warps of the CTA in their order; a thread has four dimensions of a row
-        if (piece > 0) __syncthreads();  // the last piece's results are read
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
 #pragma unroll
@@ -519,7 +657,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
             if (gid == 0) part_ml[warp][2 * tid + r] = make_float2(run.m[r], run.sum[r]);
 #pragma unroll
             for (int i = 0; i < D / 8; i += 4)
-                *(float4 *)&part[warp][2 * tid + r][gid * (D / 8) + i] = make_float4(run.o[i][r], run.o[i + 1][r], run.o[i + 2][r], run.o[i + 3][r]);
+                *(float4 *)(part(warp, 2 * tid + r) + gid * (D / 8) + i) = make_float4(run.o[i][r], run.o[i + 1][r], run.o[i + 2][r], run.o[i + 3][r]);
         }
         __syncthreads();
         auto finish = [&](int r, int c, float m, float sum, float4 v) {
@@ -544,7 +682,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
                 const float2 ml = part_ml[w][r];
                 const float f = ml.y == 0.f ? 0.f : tc::ex2(ml.x - ref);
                 sum = fmaf(ml.y, f, sum);
-                const float4 y = *(const float4 *)&part[w][r][c];
+                const float4 y = *(const float4 *)(part(w, r) + c);
                 v.x = fmaf(y.x, f, v.x), v.y = fmaf(y.y, f, v.y), v.z = fmaf(y.z, f, v.z), v.w = fmaf(y.w, f, v.w);
             }
             if (whole) {
@@ -604,18 +742,28 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
     }
 }
 
+template <typename T, int D>
+cudaError_t launch(const Ctx &ctx, const DecodeArgs &p, dim3 grid, cudaStream_t stream) {
+    const int bit = kSmemDecode + (sizeof(T) == 4);  // a context has one head dimension
+    if (!ctx.smem_ready(bit)) {
+        cudaError_t e = cudaFuncSetAttribute(decode_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<D>::kSmem);
+        if (e != cudaSuccess) return e;
+        ctx.smem_set(bit);
+    }
+    ctx.launches += 1;
+    return launch_chained(decode_kernel<T, D>, grid, dim3(kThreads), Geometry<D>::kSmem, stream, p);
+}
 template <typename T>
 cudaError_t launch_t(const Ctx &ctx, const DecodeArgs &p, dim3 grid, cudaStream_t stream) {
-    ctx.launches += 1;
     switch (p.mv.d) {
-        case 32: return launch_chained(decode_kernel<T, 32>, grid, dim3(kThreads), 0, stream, p);
-        case 64: return launch_chained(decode_kernel<T, 64>, grid, dim3(kThreads), 0, stream, p);
-        case 96: return launch_chained(decode_kernel<T, 96>, grid, dim3(kThreads), 0, stream, p);
-        case 128: return launch_chained(decode_kernel<T, 128>, grid, dim3(kThreads), 0, stream, p);
-        case 160: return launch_chained(decode_kernel<T, 160>, grid, dim3(kThreads), 0, stream, p);
-        case 192: return launch_chained(decode_kernel<T, 192>, grid, dim3(kThreads), 0, stream, p);
-        case 224: return launch_chained(decode_kernel<T, 224>, grid, dim3(kThreads), 0, stream, p);
-        case 256: return launch_chained(decode_kernel<T, 256>, grid, dim3(kThreads), 0, stream, p);
+        case 32: return launch<T, 32>(ctx, p, grid, stream);
+        case 64: return launch<T, 64>(ctx, p, grid, stream);
+        case 96: return launch<T, 96>(ctx, p, grid, stream);
+        case 128: return launch<T, 128>(ctx, p, grid, stream);
+        case 160: return launch<T, 160>(ctx, p, grid, stream);
+        case 192: return launch<T, 192>(ctx, p, grid, stream);
+        case 224: return launch<T, 224>(ctx, p, grid, stream);
+        case 256: return launch<T, 256>(ctx, p, grid, stream);
     }
     return cudaErrorInvalidValue;
 }
