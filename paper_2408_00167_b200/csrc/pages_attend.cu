@@ -59,33 +59,42 @@ __device__ __forceinline__ Request request_of(const DecodeArgs &p, int b) {
 __device__ __forceinline__ int quotient(int64_t a, int64_t b) {
     return a <= INT_MAX && b <= INT_MAX ? (int)a / (int)b : (int)(a / b);
 }
-// Equal shares: `more` CTAs have one item above `each`.
+// Equal shares: `more` CTAs have one item above `each`.  With `groups` equal groups of items and of CTAs (the units of a single
+// request) every group is shared by itself, so that no CTA has pieces of two units.
 struct Shares {
-    int64_t each;
-    int more;
-    __device__ __forceinline__ Shares(int64_t items, int ctas) {
-        each = items <= INT_MAX ? (int)items / ctas : items / ctas;
-        more = (int)(items - each * ctas);
+    int64_t each, of_group;
+    int more, ctas;
+    __device__ __forceinline__ Shares(int64_t items, int all_ctas, int groups) {
+        of_group = groups > 1 ? quotient(items, groups) : items;
+        ctas = all_ctas / groups;
+        each = of_group <= INT_MAX ? (int)of_group / ctas : of_group / ctas;
+        more = (int)(of_group - each * ctas);
     }
-    __device__ __forceinline__ int64_t begin(int c) const { return each * c + min(c, more); }
+    __device__ __forceinline__ int64_t begin(int c) const {
+        const int g = c / ctas, r = c - g * ctas;
+        return of_group * g + each * r + min(r, more);
+    }
     __device__ __forceinline__ int of(int64_t item) const {
+        const int g = item < of_group ? 0 : quotient(item, of_group);
+        item -= of_group * g;
         const int64_t big = (each + 1) * more;
-        return item < big ? quotient(item, each + 1) : more + quotient(item - big, each);
+        return g * ctas + (item < big ? quotient(item, each + 1) : more + quotient(item - big, each));
     }
 };
 
 // Where a CTA's items begin: request, and the items in front of it.  Every warp searches by itself, kScan requests to a lane.
 struct Place {
-    int b;
+    int b, groups;  // groups: of Shares
     int64_t in_front, total;
 };
 __device__ __forceinline__ Place find_items(const DecodeArgs &p) {
     const int lane = threadIdx.x & 31, batch = p.bv.batch;
-    Place place = {0, 0, 0};
+    Place place = {0, 1, 0, 0};
     if (batch == 1) {
         const Request r = request_of(p, 0);
         if (!r.u.ok && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, FINCH_DEV_BAD_BATCH);
         place.total = r.all_items();
+        if (r.units > 0 && gridDim.x % r.units == 0) place.groups = r.units;
         return place;
     }
     const bool one_step = batch <= 32 * kScan;
@@ -114,7 +123,7 @@ __device__ __forceinline__ Place find_items(const DecodeArgs &p) {
             before += __shfl_sync(0xffffffffu, incl, 31);
             if (one_step) place.total = before;
             if (pass == 1) {
-                const int64_t begin = Shares(place.total, gridDim.x).begin(blockIdx.x);
+                const int64_t begin = Shares(place.total, gridDim.x, 1).begin(blockIdx.x);
                 int hit = -1;
                 int64_t hit_at = 0;
 #pragma unroll
@@ -366,7 +375,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
     uint8_t *mine = ring + warp * Geo::kSlots * Geo::kSlot;
     auto part = [&](int w, int r) { return (float *)(ring + w * Geo::kSlots * Geo::kSlot) + r * (D + 4); };
     const Place place = find_items(p);
-    const Shares shares(place.total, gridDim.x);
+    const Shares shares(place.total, gridDim.x, place.groups);
     int64_t at = shares.begin(blockIdx.x);
     const int64_t end = shares.begin(blockIdx.x + 1);
     if (at >= end) return;
@@ -393,6 +402,32 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
         const int least = limit(0), lim[2] = {limit(2 * tid), limit(2 * tid + 1)};
 
         if (piece > 0) __syncthreads();  // the last piece's results are read: pages may take their place
+
+        // ---- full pages: a page to a warp.  Its three slots take K and V of its pages in turn: one is read, two are on their way.
+        const int *table = p.pg.table + (int64_t)b * p.pg.table_width;
+        const int page1 = min(item1, req.pages), n_mine = max(0, (page1 - (item0 + warp) + kWarps - 1) / kWarps);
+        const uint32_t mine_u = ptx::smem_u32(mine);
+        auto number_of = [&](int n) { return n < n_mine ? __ldg(table + item0 + warp + n * kWarps) : 0; };
+        auto good = [&](int number) { return number >= 0 && number < p.pg.n_pages; };
+        auto place_of = [&](int number) { return p.pg.page_head(mv, l, good(number) ? number : 0, kvh); };  // what is read of a bad one does not count
+        auto fetch = [&](int n, int number, bool is_v) {   // K or V of this warp's n-th page
+            if (n < n_mine) {
+                const uint8_t *src = (is_v ? p.pg.v : p.pg.k) + place_of(number) * Geo::kSlot;
+                const uint32_t slot = mine_u + (2 * n + is_v) % Geo::kSlots * Geo::kSlot;
+#pragma unroll
+                for (int i = 0; i < Geo::kSlot / 512; ++i) {
+                    const int x = (i * 32 + lane) * 16;
+                    copy16(slot + Geo::place(x / D, x % D), src + x);
+                }
+            }
+            copies_commit();
+        };
+        int n0 = number_of(0), n1 = number_of(1), n2 = number_of(2);
+        float k_scale = 0.f, v_scale = 0.f;
+        if (n_mine > 0) k_scale = __ldg(p.pg.k_scale + place_of(n0)), v_scale = __ldg(p.pg.v_scale + place_of(n0));
+        fetch(0, n0, false);
+        fetch(0, n0, true);
+        fetch(1, n1, false);
 
         // ---- Q: row gid's dimensions of this lane, scaled into [1, 2); up[r]: what logits of rows 2 tid + r are multiplied by
         uint32_t qh[Geo::kSteps][2], ql[kTwoParts ? Geo::kSteps : 1][2];
@@ -433,32 +468,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
         Running<D> run;
         run.clear();
 
-        // ---- full pages: a page to a warp.  Its three slots take K and V of its pages in turn: one is read, two are on their way.
-        const int *table = p.pg.table + (int64_t)b * p.pg.table_width;
         {
-            const int page1 = min(item1, req.pages), n_mine = max(0, (page1 - (item0 + warp) + kWarps - 1) / kWarps);
-            const uint32_t mine_u = ptx::smem_u32(mine);
-            auto number_of = [&](int n) { return n < n_mine ? __ldg(table + item0 + warp + n * kWarps) : 0; };
-            auto good = [&](int number) { return number >= 0 && number < p.pg.n_pages; };
-            auto place_of = [&](int number) { return p.pg.page_head(mv, l, good(number) ? number : 0, kvh); };  // what is read of a bad one does not count
-            auto fetch = [&](int n, int number, bool is_v) {   // K or V of this warp's n-th page
-                if (n < n_mine) {
-                    const uint8_t *src = (is_v ? p.pg.v : p.pg.k) + place_of(number) * Geo::kSlot;
-                    const uint32_t slot = mine_u + (2 * n + is_v) % Geo::kSlots * Geo::kSlot;
-#pragma unroll
-                    for (int i = 0; i < Geo::kSlot / 512; ++i) {
-                        const int x = (i * 32 + lane) * 16;
-                        copy16(slot + Geo::place(x / D, x % D), src + x);
-                    }
-                }
-                copies_commit();
-            };
-            int n0 = number_of(0), n1 = number_of(1), n2 = number_of(2);
-            float k_scale = 0.f, v_scale = 0.f;
-            if (n_mine > 0) k_scale = __ldg(p.pg.k_scale + place_of(n0)), v_scale = __ldg(p.pg.v_scale + place_of(n0));
-            fetch(0, n0, false);
-            fetch(0, n0, true);
-            fetch(1, n1, false);
 #pragma unroll 1
             for (int n = 0; n < n_mine; ++n) {
                 const float f[2] = {up[0] * k_scale, up[1] * k_scale};
@@ -779,10 +789,15 @@ cudaError_t launch_pages_attend(const Ctx &ctx, const PagesView &pg, const Paged
     const DecodeArgs p = {mv, pg, bv, q, out, ctx.pieces, ctx.d_status, mv.scale * kLog2e};
     const int64_t max_units = (int64_t)mv.L * mv.Hkv * ((bv.max_q * (int64_t)mv.g + kRows - 1) / kRows);
     if (max_units * kRows > INT_MAX) return cudaErrorInvalidConfiguration;
-    // every warp of a CTA a page where there are few
-    const int64_t items = max_units * bv.batch * (bv.max_len / kPage + 1);
-    int ctas = pages_ctas(ctx.sm_count);
-    if (items < (int64_t)ctas * kWarps) ctas = (int)((items + kWarps - 1) / kWarps);
+    // Every warp of a CTA a page where there are few; for a single request whole numbers of CTAs to a unit, where that takes no more
+    // than a tenth of them away.
+    const int64_t pages = (bv.max_len + kPage - 1) / kPage > 0 ? (bv.max_len + kPage - 1) / kPage : 1;
+    const int most = pages_ctas(ctx.sm_count);
+    int64_t per_unit = (pages + kWarps - 1) / kWarps;
+    if (per_unit * max_units * bv.batch > most) per_unit = most / max_units;
+    const int64_t aligned = per_unit * max_units, shared = max_units * bv.batch * ((pages + kWarps - 1) / kWarps);
+    int ctas = (int)(shared < most ? shared : most);
+    if (bv.batch == 1 && 10 * aligned >= 9 * (int64_t)ctas) ctas = (int)aligned;
     return mv.elem_bytes == 4 ? launch_t<float>(ctx, p, dim3(ctas), stream) : launch_t<__nv_bfloat16>(ctx, p, dim3(ctas), stream);
 }
 
