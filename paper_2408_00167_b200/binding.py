@@ -339,22 +339,54 @@ def finch_step_host(ctx, host_prompt_q, host_chunk_k, host_chunk_v, host_chunk_p
 
 # ------------------------------------------------------------------ rotation, attention, the paged 8-bit cache
 
-def _same(what: str, like, *tensors) -> None:
-    """Every tensor on `like`'s device and of its dtype: a kernel would read the bits of another one all the same."""
+def _views_like(what: str, like, *tensors):
+    """_views of tensors that have to be on `like`'s device and of its dtype: a kernel would read the bits of another one all the
+    same.  The checks of a call are most of what it takes on the host, hence one pass over the tensors."""
+    n = len(tensors)
+    pack = _packs.get(n)
+    if pack is None:
+        pack = _packs[n] = (struct.Struct("=" + "Qqqq" * n), C.c_char * (n * _VIEW_BYTES))
+    buf = pack[1]()
+    dtype, device = like.dtype, like.get_device()
+    fields = []
     for t in tensors:
-        if t is not None and (t.dtype != like.dtype or t.device != like.device):
-            raise ValueError(f"{what}: expected {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+        if t is None:
+            fields += (0, 0, 0, 0)
+            continue
+        if t.dtype != dtype or t.get_device() != device:
+            raise ValueError(f"{what}: expected {dtype} on {like.device}, got {t.dtype} on {t.device}")
+        st = t.stride()
+        if len(st) != 4 or (st[3] != 1 and t.shape[3] > 1):
+            raise ValueError(f"{what}: expected a [layers][heads][tokens][head_dim] tensor with head_dim contiguous")
+        fields += (t.data_ptr(), st[0], st[1], st[2])
+    pack[0].pack_into(buf, 0, *fields)
+    return buf, C.addressof(buf)
 
 
-def _typed(what: str, dtype: str, like, *tensors) -> None:
-    for t in tensors:
-        if t is not None and (str(t.dtype) != "torch." + dtype or t.device != like.device or not t.is_contiguous()):
-            raise ValueError(f"{what}: expected a contiguous torch.{dtype} tensor on {like.device}, got {t.dtype} on {t.device}")
+def _array(what: str, t, dtype, like, shape):
+    """Address of a contiguous tensor of the given dtype and shape on `like`'s device; None: none."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.get_device() != like.get_device() or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {like.device}, got {t.dtype} of "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr() or None
 
 
-def _shape(what: str, t, shape) -> None:
-    if t is not None and tuple(t.shape) != tuple(shape):
+def _same_shape(what: str, t, shape) -> None:
+    if t.shape != shape:
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+_dtypes = None
+
+
+def _i32_f32():
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = torch.int32, torch.float32
+    return _dtypes
 
 
 def finch_rope_frequencies(rotary_dim: int, theta: float = 10000.0, scaling: int = FINCH_ROPE_PLAIN, factor: float = 1.0,
@@ -384,26 +416,22 @@ def finch_rotate(ctx, q, k, pos, out_q, out_k, rope: Optional[finch_rope] = None
     """Norm (with weights) and rotation (with rope and positions) of q and k, [n_layers][heads][tokens][head_dim]; either may be
     None, together with its output."""
     like = q if q is not None else k
-    if like is None:
-        raise ValueError("finch_rotate: neither q nor k")
-    _same("finch_rotate", like, q, k, out_q, out_k, q_weight, k_weight)
-    _typed("finch_rotate: pos", "int32", like, pos)
-    L, _, tokens, d = like.shape
-    for x, out, w in ((q, out_q, q_weight), (k, out_k, k_weight)):
-        if (x is None) != (out is None):
-            raise ValueError("finch_rotate: a tensor and its output come together")
-        if x is not None:
-            _shape("finch_rotate", x, (L, x.shape[1], tokens, d))
-            _shape("finch_rotate: output", out, x.shape)
-        if w is not None and not w.is_contiguous():
-            raise ValueError("finch_rotate: weights are contiguous [n_layers][head_dim]")
-        _shape("finch_rotate: weight", w, (L, d))
-    if pos is not None:
-        _shape("finch_rotate: pos", pos, (tokens,))
-    keep, v = _views(q, k, out_q, out_k)
-    z = _VIEW_BYTES
-    _check(load().finch_rotate(ctx, v, v + z, tokens, _ptr(pos), _rope(rope), _ptr(q_weight), _ptr(k_weight), eps, v + 2 * z,
-                               v + 3 * z, _stream(stream)), "finch_rotate")
+    if like is None or (q is None) != (out_q is None) or (k is None) != (out_k is None):
+        raise ValueError("finch_rotate: q, k or both, each with its output")
+    keep, v = _views_like("finch_rotate", like, q, k, out_q, out_k)
+    shape = like.shape
+    L, _, tokens, d = shape
+    if q is not None:
+        _same_shape("finch_rotate: out_q", out_q, shape)
+    if k is not None:
+        if k is not like and (k.shape[0] != L or k.shape[2] != tokens or k.shape[3] != d):
+            raise ValueError(f"finch_rotate: k is {tuple(k.shape)}, q {tuple(shape)}")
+        _same_shape("finch_rotate: out_k", out_k, k.shape)
+    z, dtype = _VIEW_BYTES, like.dtype
+    _check(load().finch_rotate(ctx, v, v + z, tokens, _array("finch_rotate: pos", pos, _i32_f32()[0], like, (tokens,)), _rope(rope),
+                               _array("finch_rotate: q_weight", q_weight, dtype, like, (L, d)),
+                               _array("finch_rotate: k_weight", k_weight, dtype, like, (L, d)), eps, v + 2 * z, v + 3 * z,
+                               _stream(stream)), "finch_rotate")
 
 
 def finch_attend_workspace_bytes(ctx, batch: Batch) -> int:
@@ -415,14 +443,13 @@ def finch_attend_workspace_bytes(ctx, batch: Batch) -> int:
 def finch_attend(ctx, q, cache_k, cache_v, chunk_k, chunk_v, batch: Batch, out, row_lse=None, causal: bool = True, ws=None,
                  stream=None) -> None:
     """Attention of the packed query rows over [cache ; chunk] (see the header); `out` has q's shape."""
-    _same("finch_attend", q, cache_k, cache_v, chunk_k, chunk_v, out)
-    _typed("finch_attend: row_lse", "float32", q, row_lse)
-    _shape("finch_attend: out", out, q.shape)
-    _shape("finch_attend: row_lse", row_lse, q.shape[:3])
-    keep, v = _views(q, cache_k, cache_v, chunk_k, chunk_v, out)
+    keep, v = _views_like("finch_attend", q, q, cache_k, cache_v, chunk_k, chunk_v, out)
+    shape = q.shape
+    _same_shape("finch_attend: out", out, shape)
     z = _VIEW_BYTES
-    _check(load().finch_attend(ctx, v, v + z, v + 2 * z, v + 3 * z, v + 4 * z, C.addressof(batch.c), int(bool(causal)), v + 5 * z,
-                               _ptr(row_lse), _ptr(ws), _nbytes(ws), _stream(stream)), "finch_attend")
+    _check(load().finch_attend(ctx, v, v + z, v + 2 * z, v + 3 * z, v + 4 * z, C.addressof(batch.c), 1 if causal else 0, v + 5 * z,
+                               _array("finch_attend: row_lse", row_lse, _i32_f32()[1], q, shape[:3]), _ptr(ws), _nbytes(ws),
+                               _stream(stream)), "finch_attend")
 
 
 @dataclass
@@ -494,15 +521,13 @@ def make_paged_batch(lengths: Sequence[int], q_off: Optional[Sequence[int]] = No
 def finch_pages_append(ctx, pages: Pages, batch: PagedBatch, new_k, new_v, out_len=None, rope: Optional[finch_rope] = None, pos=None,
                        stream=None) -> None:
     """Rows of new_k (turned to their positions with rope) and new_v behind each request's tokens (see the header)."""
-    _same("finch_pages_append", pages.tensors[4], new_k, new_v)
-    _typed("finch_pages_append: out_len and pos", "int32", new_k, out_len, pos)
-    if pos is not None:
-        _shape("finch_pages_append: pos", pos, (new_k.shape[2],))
-    if out_len is not None and out_len.numel() < batch.c.batch:
-        raise ValueError("finch_pages_append: out_len holds a length for each request")
-    keep, v = _views(new_k, new_v)
-    _check(load().finch_pages_append(ctx, C.addressof(pages.c), C.addressof(batch.c), v, v + _VIEW_BYTES, _rope(rope), _ptr(pos),
-                                     _ptr(out_len), _stream(stream)), "finch_pages_append")
+    like = pages.tensors[4]
+    keep, v = _views_like("finch_pages_append", like, new_k, new_v)
+    i32 = _i32_f32()[0]
+    _check(load().finch_pages_append(ctx, C.addressof(pages.c), C.addressof(batch.c), v, v + _VIEW_BYTES, _rope(rope),
+                                     None if pos is None else _array("finch_pages_append: pos", pos, i32, like, new_k.shape[2:3]),
+                                     _array("finch_pages_append: out_len", out_len, i32, like, (batch.c.batch,)), _stream(stream)),
+           "finch_pages_append")
 
 
 def finch_pages_workspace_bytes(ctx, batch: PagedBatch) -> int:
@@ -513,10 +538,9 @@ def finch_pages_workspace_bytes(ctx, batch: PagedBatch) -> int:
 
 def finch_pages_attend(ctx, pages: Pages, batch: PagedBatch, q, out, row_lse=None, ws=None, stream=None) -> None:
     """Attention of each request's newest tokens over its paged cache (see the header); `out` has q's shape."""
-    _same("finch_pages_attend", pages.tensors[4], q, out)
-    _typed("finch_pages_attend: row_lse", "float32", q, row_lse)
-    _shape("finch_pages_attend: out", out, q.shape)
-    _shape("finch_pages_attend: row_lse", row_lse, q.shape[:3])
-    keep, v = _views(q, out)
-    _check(load().finch_pages_attend(ctx, C.addressof(pages.c), C.addressof(batch.c), v, v + _VIEW_BYTES, _ptr(row_lse), _ptr(ws),
+    keep, v = _views_like("finch_pages_attend", pages.tensors[4], q, out)
+    shape = q.shape
+    _same_shape("finch_pages_attend: out", out, shape)
+    _check(load().finch_pages_attend(ctx, C.addressof(pages.c), C.addressof(batch.c), v, v + _VIEW_BYTES,
+                                     _array("finch_pages_attend: row_lse", row_lse, _i32_f32()[1], q, shape[:3]), _ptr(ws),
                                      _nbytes(ws), _stream(stream)), "finch_pages_attend")

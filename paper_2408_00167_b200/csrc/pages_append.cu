@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kRowsPass * LPR, (sizeof(T) == 2 && !ROPE ? 76
                     if (!__any_sync(0xffffffffu, fresh)) continue;
                     float y[kRotVec];
                     x[a].get(y);
-                    rotate8<LPR, true>(y, table + (fresh ? slot : from) * half, at, rope.rotary_dim, rope.pairing);
+                    rotate8<LPR>(y, table + (fresh ? slot : from) * half, at, rope.rotary_dim, rope.pairing);
                     if (fresh) x[a].set(y);  // a row waits, and is quantised, in the model's type
                 }
             }

@@ -60,6 +60,12 @@ struct Eight<float> {
     __device__ __forceinline__ void get(float (&x)[kRotVec]) const {
         x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
     }
+    __device__ __forceinline__ void from_lane(int lane) {
+        a.x = __shfl_sync(0xffffffffu, a.x, lane), a.y = __shfl_sync(0xffffffffu, a.y, lane);
+        a.z = __shfl_sync(0xffffffffu, a.z, lane), a.w = __shfl_sync(0xffffffffu, a.w, lane);
+        b.x = __shfl_sync(0xffffffffu, b.x, lane), b.y = __shfl_sync(0xffffffffu, b.y, lane);
+        b.z = __shfl_sync(0xffffffffu, b.z, lane), b.w = __shfl_sync(0xffffffffu, b.w, lane);
+    }
     // The bits of the largest magnitude so far (as unsigned numbers magnitudes are in order, infinities and NaN behind all others).
     __device__ __forceinline__ void fold_magnitude(uint32_t &top) const {
         float x[kRotVec];
@@ -90,6 +96,10 @@ struct Eight<__nv_bfloat16> {
             x[2 * i] = __uint_as_float(w[i] << 16);
             x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
+    }
+    __device__ __forceinline__ void from_lane(int lane) {
+        v.x = __shfl_sync(0xffffffffu, v.x, lane), v.y = __shfl_sync(0xffffffffu, v.y, lane);
+        v.z = __shfl_sync(0xffffffffu, v.z, lane), v.w = __shfl_sync(0xffffffffu, v.w, lane);
     }
     // two 16-bit lanes of magnitudes; `magnitude` gives the larger one as the bits of an fp32 number
     __device__ __forceinline__ void fold_magnitude(uint32_t &top) const {
@@ -129,8 +139,8 @@ __device__ __forceinline__ float turn_exact(float a, float c, float b, float s) 
 
 // Turns the 8 elements that lane `at` of a row's LPR lanes holds; cs is the row's part of the table.  Every lane of the
 // warp takes part.  rotary_dim is a multiple of 16, so that an element's partner half the rotary dimensions on has the same
-// place in another lane's eight.  EXACT: the sum of the two products is rounded once.
-template <int LPR, bool EXACT>
+// place in another lane's eight.  The sum of the two products is rounded once.
+template <int LPR>
 __device__ __forceinline__ void rotate8(float (&x)[kRotVec], const float2 *cs, int at, int rotary_dim, int pairing) {
     const int e0 = at * kRotVec, half = rotary_dim / 2;
     if (pairing) {
@@ -139,8 +149,8 @@ __device__ __forceinline__ void rotate8(float (&x)[kRotVec], const float2 *cs, i
         for (int i = 0; i < kRotVec; i += 2) {
             const float2 t = cs[(e0 + i) / 2];
             const float a = x[i], b = x[i + 1];
-            x[i] = EXACT ? turn_exact<true>(a, t.x, b, t.y) : a * t.x - b * t.y;
-            x[i + 1] = EXACT ? turn_exact<false>(a, t.y, b, t.x) : a * t.y + b * t.x;
+            x[i] = turn_exact<true>(a, t.x, b, t.y);
+            x[i + 1] = turn_exact<false>(a, t.y, b, t.x);
         }
     } else {
         const int lane = threadIdx.x & 31, first = lane - at, step = half / kRotVec;
@@ -152,9 +162,9 @@ __device__ __forceinline__ void rotate8(float (&x)[kRotVec], const float2 *cs, i
             if (turns) {
                 const float2 t = cs[low ? e0 + i : e0 + i - half];
                 if (low)
-                    x[i] = EXACT ? turn_exact<true>(x[i], t.x, other, t.y) : x[i] * t.x - other * t.y;
+                    x[i] = turn_exact<true>(x[i], t.x, other, t.y);
                 else
-                    x[i] = EXACT ? turn_exact<false>(other, t.y, x[i], t.x) : other * t.y + x[i] * t.x;
+                    x[i] = turn_exact<false>(other, t.y, x[i], t.x);
             }
         }
     }
