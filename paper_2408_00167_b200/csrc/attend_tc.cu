@@ -28,6 +28,7 @@ using namespace tc;
 constexpr int kTcThreads = 384;      // 4 control warps, 2 x 4 softmax warps
 constexpr float kGrowth = 8.f;       // binary orders that a row's maximum may grow before O is scaled
 constexpr int kTileRows = 128;
+constexpr int kMaxCluster = 8;
 
 struct TcArgs {
     ModelView mv;
@@ -36,6 +37,7 @@ struct TcArgs {
     int *status;
     int causal, heads, tok, chunks, row_tiles;  // query heads and tokens of a row tile; tiles of heads per KV head; CTAs along the tokens
     int two_tiles;                               // streams are two row tiles (else: one tile's even and odd key tiles)
+    int cluster;                                 // consecutive splits whose CTAs are a cluster and add their results there
     float scale2;
 };
 
@@ -56,6 +58,44 @@ struct Barriers {
     uint64_t ragged[2], clean[2];  // the cache's, the chunk's last V tile: on its way, cleared behind its rows
 };
 
+// Where one row's result goes: the output and its log-sum-exp, or (unnormalised) the partial results of a split.
+struct Row {
+    const TcArgs &p;
+    int64_t row, slot;
+    __nv_bfloat16 *dst;
+    bool writes, partial;
+    float inv;
+    __device__ __forceinline__ Row(const TcArgs &args, const UnitInfo &u, int l, int h, int t, bool w, int split) : p(args), writes(w), inv(1.f) {
+        partial = p.out.splits > p.cluster;
+        row = w ? attend_row(p.mv, p.bv.total_q, l, h, u.q0 + t) : 0;
+        slot = split * ((int64_t)p.mv.L * p.mv.Hq * p.bv.total_q) + row;
+        dst = (__nv_bfloat16 *)p.out.ptr + (int64_t)l * p.out.stride_layer + (int64_t)h * p.out.stride_head + (int64_t)(u.q0 + t) * p.out.stride_tok;
+    }
+    __device__ __forceinline__ void finish(float m, float l, bool notes = true) {
+        if (!writes) return;
+        if (partial) {
+            if (notes) p.out.part_ml[slot] = make_float2(m, l);
+            return;
+        }
+        float lse;
+        inv = attend_finish(m, l, p.bv.self_lse, row, lse);
+        if (notes && p.out.row_lse) p.out.row_lse[row] = lse;
+    }
+    __device__ __forceinline__ void put(int c, const float *y) {  // eight columns
+        if (!writes) return;
+        if (partial) {
+            float *po = p.out.part_o + slot * p.mv.d + c;
+            *(float4 *)po = make_float4(y[0], y[1], y[2], y[3]);
+            *(float4 *)(po + 4) = make_float4(y[4], y[5], y[6], y[7]);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(y[2 * k + 1] * inv), "f"(y[2 * k] * inv));
+            *(uint4 *)(dst + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+};
+
 template <int DP>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TcArgs p) {
     using Lay = Layout<DP>;
@@ -66,6 +106,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     __shared__ int limit_s[2];
     uint8_t *smem = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     uint8_t *q_smem = smem, *ring = smem + 2 * Lay::kTile;
+    // a stream's result in the ring's place: [DP] columns of O, m, l, of 128 rows each
+    auto box = [&](int s) { return (float *)ring + s * (DP + 2) * 128; };
+    static_assert(2 * (DP + 2) * 128 * 4 <= Lay::kStages * Lay::kTile, "results take the ring's place");
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     dependency_wait();
     const ModelView &mv = p.mv;
@@ -308,13 +351,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         if (count[s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.o_full[s], 0, &abort_flag));
         tc_fence_after();
         const float m2 = m * p.scale2;   // the reference in base-2 logits (-inf: none of the row's keys)
-        const int64_t row = live ? attend_row(mv, p.bv.total_q, l, h0 + hr, u.q0 + tr) : 0;
+        const bool shares = p.cluster > 1 || (!p.two_tiles && count[1] > 0);  // the result meets others in shared memory
+        if (shares) {
+            // the pages' place is free when the other stream's MMAs are complete, too
+            if (count[1 - s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.o_full[1 - s], 0, &abort_flag));
+            tc_fence_after();
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+        }
         float scale_o = 1.f, total = sum, ref = m2, other = 0.f;
-        float *swap = (float *)ring;     // [DP + 2][128]: the second stream's O, m, l
-        bool writes = live;
+        float *mine = box(p.two_tiles ? s : 0);
         if (!p.two_tiles && count[1] > 0) {
-            // every MMA that reads the ring is complete before the second stream's result goes there
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.o_full[1 - s], 0, &abort_flag));
             if (s == 1) {
 #pragma unroll 1
                 for (int c = 0; c < DP / 32; ++c) {
@@ -322,14 +368,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     tmem_ld_issue(ot + c * 32, o);
                     tmem_ld_wait(o);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) swap[(c * 32 + e) * 128 + r] = __uint_as_float(o[e]);
+                    for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * 128 + r] = __uint_as_float(o[e]);
                 }
-                swap[DP * 128 + r] = m2;
-                swap[(DP + 1) * 128 + r] = sum;
+                mine[DP * 128 + r] = m2;
+                mine[(DP + 1) * 128 + r] = sum;
             }
             asm volatile("bar.sync 1, 256;" ::: "memory");
             if (s == 0) {
-                const float mo = swap[DP * 128 + r], lo = swap[(DP + 1) * 128 + r];
+                const float mo = mine[DP * 128 + r], lo = mine[(DP + 1) * 128 + r];
                 ref = fmaxf(sum == 0.f ? -INFINITY : m2, lo == 0.f ? -INFINITY : mo);
                 const float base = ref == -INFINITY ? 0.f : ref;
                 scale_o = sum == 0.f ? 0.f : exp2f(m2 - base);
@@ -337,15 +383,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 total = sum * scale_o + lo * other;
             }
         }
-        if (!p.two_tiles && s == 1) writes = false;
-        float lse = 0.f, inv = 1.f;
-        const bool partial = p.out.splits > 1;
-        if (writes && !partial) inv = attend_finish(ref, total, p.bv.self_lse, row, lse);
-        const int64_t slot = split * ((int64_t)mv.L * mv.Hq * p.bv.total_q) + row;
-        __nv_bfloat16 *dst = (__nv_bfloat16 *)p.out.ptr + (int64_t)l * p.out.stride_layer + (int64_t)(h0 + hr) * p.out.stride_head +
-                             (int64_t)(u.q0 + tr) * p.out.stride_tok;
+        const bool holds = p.two_tiles || s == 0;   // the row's result is in these warps
+        Row row(p, u, l, h0 + hr, tr, live && holds, split / p.cluster);
+        if (holds && p.cluster == 1) row.finish(ref, total);
 #pragma unroll 1
-        for (int c = 0; c < mv.d / 32 && (p.two_tiles || s == 0); ++c) {
+        for (int c = 0; c < (p.cluster > 1 ? DP : mv.d) / 32 && holds; ++c) {
             uint32_t o[32];
             if (count[s] > 0) {
                 tmem_ld_issue(ot + c * 32, o);
@@ -355,31 +397,68 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
                 y[e] = count[s] > 0 && sum != 0.f ? __uint_as_float(o[e]) * scale_o : 0.f;
-                if (other != 0.f) y[e] = fmaf(swap[(c * 32 + e) * 128 + r], other, y[e]);
-                y[e] *= inv;
+                if (other != 0.f) y[e] = fmaf(mine[(c * 32 + e) * 128 + r], other, y[e]);
             }
-            if (writes && partial) {
-                float *po = p.out.part_o + slot * mv.d + c * 32;
+            if (p.cluster > 1) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) *(float4 *)(po + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
-            } else if (writes) {
+                for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * 128 + r] = y[e];
+            } else {
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(y[e + 2 * k + 1]), "f"(y[e + 2 * k]));
-                    *(uint4 *)(dst + c * 32 + e) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+                for (int e = 0; e < 32; e += 8) row.put(c * 32 + e, &y[e]);
             }
             __syncwarp();
         }
-        if (writes) {
-            if (partial)
-                p.out.part_ml[slot] = make_float2(ref, total);
-            else if (p.out.row_lse)
-                p.out.row_lse[row] = lse;
-        }
+        if (holds && p.cluster > 1) mine[DP * 128 + r] = ref, mine[(DP + 1) * 128 + r] = total;
         tc_fence_before();
+    }
+    if (p.cluster > 1) {
+        // ---- the splits of the cluster: every CTA adds all of them for some columns, from their shared memory
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        if (warp >= 4) {
+            const int rank = split % p.cluster, boxes = p.two_tiles ? 2 : 1;
+            for (int task = warp - 4;; task += 8) {
+                const int x = task / 4 % boxes, c0 = (rank + task / 4 / boxes * p.cluster) * 8, r = task % 4 * 32 + lane;
+                if (c0 >= mv.d) break;
+                const uint32_t at = smem_u32(box(x)) + r * 4;
+                const int hr = r / p.tok, tr = t0 + x * p.tok + r % p.tok;
+                Row row(p, u, l, h0 + hr, tr, hr < n_heads && tr < u.n_q, split / p.cluster);
+                float m[kMaxCluster], f[kMaxCluster], ref = -INFINITY, total = 0.f, y[8];
+#pragma unroll
+                for (int j = 0; j < kMaxCluster; ++j) {
+                    m[j] = -INFINITY, f[j] = 0.f;
+                    if (j < p.cluster) {
+                        m[j] = ld_remote_f32(map_to_rank(at + DP * 512, j));
+                        f[j] = ld_remote_f32(map_to_rank(at + (DP + 1) * 512, j));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kMaxCluster; ++j)
+                    if (f[j] != 0.f) ref = fmaxf(ref, m[j]);
+                const float base = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+                for (int j = 0; j < kMaxCluster; ++j) {
+                    const float g = f[j] == 0.f ? 0.f : ex2(m[j] - base);
+                    total = fmaf(f[j], g, total);
+                    f[j] = g;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = 0.f;
+#pragma unroll
+                for (int j = 0; j < kMaxCluster; ++j)
+                    if (j < p.cluster) {
+                        const uint32_t from = map_to_rank(at + c0 * 512, j);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = fmaf(ld_remote_f32(from + e * 512), f[j], y[e]);
+                    }
+                row.finish(ref, total, c0 == 0);
+                row.put(c0, y);
+            }
+        }
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();   // nobody reads this CTA's shared memory any more
     }
     __syncthreads();
     if (warp == 1) {
@@ -398,7 +477,7 @@ cudaError_t launch(const Ctx &ctx, const Maps &maps, const TcArgs &p, dim3 grid,
         ctx.smem_set(bit);
     }
     ctx.launches += 1;
-    return launch_chained(attend_tc_kernel<DP>, grid, dim3(kTcThreads), Layout<DP>::kBytes, stream, maps, p);
+    return launch_chained_cluster(attend_tc_kernel<DP>, p.cluster, grid, dim3(kTcThreads), Layout<DP>::kBytes, stream, maps, p);
 }
 
 // A map of a row tile's queries: one box is `tok` tokens of `heads` heads.
@@ -416,6 +495,31 @@ bool make_q_map(CUtensorMap *map, const TensorView &t, int d, int64_t tokens, in
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Key splits of a call of `units` CTAs with `tiles` key tiles at most: first the CTAs of a cluster, then, for few rows and long
+// contexts, several clusters whose results merge_splits adds.  A key tile takes a CTA about a microsecond (half of that with two
+// streams on one row tile), the cluster's sum about three, a merge of clusters about five.
+void choose_splits(int sms, int64_t units, int tiles, int two_tiles, size_t room, int &cluster, int &splits) {
+    cluster = splits = 1;
+    const double tile_us = two_tiles ? 1.0 : 0.5;
+    auto waves = [&](int64_t ctas) { return (double)((ctas + sms - 1) / sms); };
+    double best = waves(units) * tiles * tile_us;
+    for (int c = 2; c <= kMaxCluster; ++c) {
+        // clusters of c CTAs that a device of GPCs of 16 to 18 SMs holds at a time
+        const int64_t at_once = (int64_t)(sms / 18) * (16 / c) * c;
+        if (units * c > at_once || tiles < 2 * c) break;
+        const double t = (double)((tiles + c - 1) / c) * tile_us + 3.0;
+        if (t < best) best = t, cluster = splits = c;
+    }
+    if (cluster == kMaxCluster) {
+        for (int g = 2; g <= kAttendMaxSplits && (size_t)g <= room; ++g) {
+            const int c = cluster * g;
+            if (units * c > (int64_t)(sms / 18) * 16 || tiles < 2 * c) break;
+            const double t = (double)((tiles + c - 1) / c) * tile_us + 8.0;
+            if (t < best) best = t, splits = c;
+        }
+    }
+}
+
 }  // namespace
 
 bool attend_tc_supported(const Ctx &ctx) { return ctx.cfg.dtype == FINCH_BF16 && ctx.model.d <= 128; }
@@ -424,7 +528,7 @@ cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorVi
                              const TensorView &hv, const BatchView &bv, int causal, AttendOut out, size_t partial_rows, cudaStream_t stream) {
     if (bv.batch == 0 || bv.max_q == 0) return cudaSuccess;
     const ModelView &mv = ctx.model;
-    TcArgs p = {mv, bv, out, ctx.d_status, causal, 0, 0, 0, 0, 0, mv.scale * kLog2e};
+    TcArgs p = {mv, bv, out, ctx.d_status, causal, 0, 0, 0, 0, 0, 1, mv.scale * kLog2e};
     p.heads = mv.g < kTileRows ? mv.g : kTileRows;
     p.tok = kTileRows / p.heads;
     p.chunks = (mv.g + p.heads - 1) / p.heads;
@@ -446,14 +550,13 @@ cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorVi
     const int64_t units = (int64_t)mv.L * mv.Hkv * p.chunks;
     const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
     const int key_tiles = (bv.max_cache + kTileRows - 1) / kTileRows + (bv.max_chunk + kTileRows - 1) / kTileRows;
-    int splits = attend_splits(units * p.row_tiles * bv.batch, ctx.sm_count, key_tiles, 2);
-    while (splits > 1 && splits * rows > partial_rows) --splits;
-    p.out.splits = splits;
-    const int64_t ctas = units * splits * p.row_tiles;
+    choose_splits(ctx.sm_count, units * p.row_tiles * bv.batch, key_tiles, p.two_tiles, partial_rows / (rows > 0 ? rows : 1), p.cluster, p.out.splits);
+    const int64_t ctas = units * p.out.splits * p.row_tiles;
     if (ctas > INT_MAX) return cudaErrorInvalidConfiguration;
     const dim3 grid((unsigned)ctas, bv.batch);
     cudaError_t e = mv.d <= 64 ? launch<64>(ctx, maps, p, grid, stream) : launch<128>(ctx, maps, p, grid, stream);
-    if (e == cudaSuccess && splits > 1) e = launch_merge_splits(ctx, bv, p.out, stream);
+    p.out.splits /= p.cluster;
+    if (e == cudaSuccess && p.out.splits > 1) e = launch_merge_splits(ctx, bv, p.out, stream);
     return e;
 }
 
