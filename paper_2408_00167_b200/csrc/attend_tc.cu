@@ -45,6 +45,11 @@ struct Maps {
     CUtensorMap q, ck, cv, hk, hv;
 };
 
+template <int S>
+struct Stream {
+    static constexpr int value = S;
+};
+
 template <int DP>
 struct Layout {
     static constexpr int kSlabs = DP / 64;
@@ -175,7 +180,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     // the last stream to use a tile frees it
     auto frees = [&](int s, int t) { return !p.two_tiles || s == 1 || t >= count[1]; };
     constexpr int kStages = Lay::kStages;
-    const uint32_t s_col[2] = {tmem, tmem + 128}, o_col[2] = {tmem + 256, tmem + 256 + DP};
 
     if (warp < 4) regs_dec<56>();
     if (warp == 0) {
@@ -186,13 +190,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
             for (int s = 0; s < q_tiles; ++s)
                 for (int c = 0; c < Lay::kSlabs; ++c)
                     tma_load_4d(q_smem + s * Lay::kTile + c * kSlabBytes, &maps.q, &bar.q_full, c * 64, u.q0 + t0 + s * p.tok, h0, l);
-            int item = 0;
+            int item = 0, slot = 0;
+            uint32_t ph = 1;   // of the slot's last reader: the first round waits for nobody
             bool ok = true;
             for (int t = 0; t < n_tiles && ok; ++t) {
                 const KeyTile kt = key_tile(u, begin + t);
-                for (int v = 0; v < 2; ++v, ++item) {
-                    const int slot = item % kStages;
-                    if (item >= kStages && !(ok = mbar_wait(&bar.empty[slot], (item / kStages - 1) & 1, &abort_flag))) break;
+                for (int v = 0; v < 2; ++v, ++item, slot = slot + 1 == kStages ? (ph ^= 1, 0) : slot + 1) {
+                    if (item >= kStages && !(ok = mbar_wait(&bar.empty[slot], ph, &abort_flag))) break;
                     mbar_expect_tx(&bar.full[slot], Lay::kTile);
                     const CUtensorMap *map = kt.is_chunk ? (v ? &maps.hv : &maps.hk) : (v ? &maps.cv : &maps.ck);
                     for (int c = 0; c < Lay::kSlabs; ++c)
@@ -206,49 +210,87 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         }
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issuer
-        if (lane == 0 && n_tiles > 0) {
+        // The whole warp keeps the control flow, so that addresses and descriptors are warp-uniform; one lane issues.  This warp's
+        // instructions are on the path of both streams: everything that is the same for every tile is formed in front of the loop.
+        if (n_tiles > 0) {
             constexpr uint32_t idesc_s = idesc_bf16_f32(128, 128), idesc_o = idesc_bf16_f32(128, DP) | kIdescBMn;
-            bool ok = mbar_wait(&bar.q_full, 0, &abort_flag);
-            const uint32_t ring_u = smem_u32(ring), q_u = smem_u32(q_smem);
-            auto issue_s = [&](int s, int i) {
-                const int t = tile_of(s, i), item = 2 * t, slot = item % kStages;
-                if (!mbar_wait(&bar.full[slot], (item / kStages) & 1, &abort_flag)) return false;
-                tc_fence_after();
-                const uint32_t qa = q_u + (p.two_tiles ? s : 0) * Lay::kTile, ka = ring_u + slot * Lay::kTile;
+            constexpr uint32_t kTile16 = Lay::kTile / 16;   // descriptors count 16 bytes
+            auto agree = [](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };
+            bool ok = agree(mbar_wait(&bar.q_full, 0, &abort_flag));
+            const uint32_t q_u = smem_u32(q_smem), ring_u = smem_u32(ring);
+            const uint64_t qd0 = smem_desc_sw128(q_u), qd[2] = {qd0, p.two_tiles ? qd0 + kTile16 : qd0};
+            const uint64_t kd = smem_desc_sw128(ring_u), vd = smem_desc_sw128_mn(ring_u, kSlabBytes);
+            // the tiles whose V rows are cleared behind the last token: the cache's last, the chunk's last
+            const int ragged0 = u.c % kTileRows ? cache_tiles - 1 - begin : -1;
+            const int ragged1 = u.m % kTileRows ? cache_tiles + (u.m + kTileRows - 1) / kTileRows - 1 - begin : -1;
+            const int step = p.two_tiles ? 2 : 4;           // items from a stream's tile to its next
+            // slot and phase of each stream's next K and V item
+            int k_slot[2], v_slot[2], tile_k[2], tile_v[2];
+            uint32_t k_ph[2] = {0, 0}, v_ph[2] = {0, 0}, p_ph[2] = {0, 0};
 #pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t at = (k / 4) * kSlabBytes + (k % 4) * 32;
-                    if (k == 0)
-                        umma_bf16_first(s_col[s], smem_desc_sw128(qa + at), smem_desc_sw128(ka + at), idesc_s);
-                    else
-                        umma_bf16_acc(s_col[s], smem_desc_sw128(qa + at), smem_desc_sw128(ka + at), idesc_s);
+            for (int s = 0; s < 2; ++s) {
+                tile_k[s] = tile_v[s] = tile_of(s, 0);
+                k_slot[s] = 2 * tile_k[s], v_slot[s] = k_slot[s] + 1;   // below kStages
+            }
+            auto issue_s = [&](auto stream) {
+                constexpr int s = decltype(stream)::value;
+                if (!agree(mbar_wait_now(&bar.full[k_slot[s]], k_ph[s], &abort_flag))) return false;
+                tc_fence_after();
+                const uint64_t b_desc = kd + k_slot[s] * kTile16;
+                const bool last = frees(s, tile_k[s]);
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const uint32_t at = ((k / 4) * kSlabBytes + (k % 4) * 32) / 16;
+                        if (k == 0)
+                            umma_bf16_first(tmem + s * 128, qd[s] + at, b_desc + at, idesc_s);
+                        else
+                            umma_bf16_acc(tmem + s * 128, qd[s] + at, b_desc + at, idesc_s);
+                    }
+                    umma_commit(&bar.s_full[s]);
+                    if (last) umma_commit(&bar.empty[k_slot[s]]);
                 }
-                umma_commit(&bar.s_full[s]);
-                if (frees(s, t)) umma_commit(&bar.empty[slot]);
+                __syncwarp();
+                tile_k[s] += step / 2;
+                k_slot[s] += step;
+                if (k_slot[s] >= kStages) k_slot[s] -= kStages, k_ph[s] ^= 1;
                 return true;
             };
-            auto issue_o = [&](int s, int i) {
-                const int t = tile_of(s, i), item = 2 * t + 1, slot = item % kStages;
-                if (!mbar_wait(&bar.p_full[s], i & 1, &abort_flag)) return false;
-                if (!mbar_wait(&bar.full[slot], (item / kStages) & 1, &abort_flag)) return false;
-                const KeyTile kt = key_tile(u, begin + t);
-                if (kt.valid < kTileRows && !mbar_wait(&bar.clean[kt.is_chunk], 0, &abort_flag)) return false;
+            auto issue_o = [&](auto stream, int i) {
+                constexpr int s = decltype(stream)::value;
+                const int t = tile_v[s];
+                if (!agree(mbar_wait_now(&bar.full[v_slot[s]], v_ph[s], &abort_flag))) return false;
+                if (t == ragged0 && !agree(mbar_wait_now(&bar.clean[0], 0, &abort_flag))) return false;
+                if (t == ragged1 && !agree(mbar_wait_now(&bar.clean[1], 0, &abort_flag))) return false;
+                if (!agree(mbar_wait_now(&bar.p_full[s], p_ph[s], &abort_flag))) return false;
                 tc_fence_after();
-                const uint32_t va = ring_u + slot * Lay::kTile;
+                const uint64_t b_desc = vd + v_slot[s] * kTile16;
+                const bool last = frees(s, t), end = i + 1 == count[s];
+                if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < kTileRows / 16; ++k)
-                    umma_bf16_tmem(o_col[s], s_col[s] + k * 8, smem_desc_sw128_mn(va + k * 2048, kSlabBytes), idesc_o, i > 0 || k > 0);
-                if (frees(s, t)) umma_commit(&bar.empty[slot]);
-                if (i + 1 == count[s]) umma_commit(&bar.o_full[s]);
+                    for (int k = 0; k < kTileRows / 16; ++k)
+                        umma_bf16_tmem(tmem + 256 + s * DP, tmem + s * 128 + k * 8, b_desc + k * (2048 / 16), idesc_o, i > 0 || k > 0);
+                    if (last) umma_commit(&bar.empty[v_slot[s]]);
+                    if (end) umma_commit(&bar.o_full[s]);
+                }
+                __syncwarp();
+                p_ph[s] ^= 1;
+                tile_v[s] += step / 2;
+                v_slot[s] += step;
+                if (v_slot[s] >= kStages) v_slot[s] -= kStages, v_ph[s] ^= 1;
                 return true;
             };
-            for (int s = 0; s < 2 && ok; ++s)
-                if (count[s] > 0) ok = issue_s(s, 0);
-            for (int i = 0; ok && i < max(count[0], count[1]); ++i)
-                for (int s = 0; s < 2 && ok; ++s) {
-                    if (i < count[s]) ok = issue_o(s, i);
-                    if (ok && i + 1 < count[s]) ok = issue_s(s, i + 1);
-                }
+            const Stream<0> s0;
+            const Stream<1> s1;
+            if (ok && count[0] > 0) ok = issue_s(s0);
+            if (ok && count[1] > 0) ok = issue_s(s1);
+            const int most = max(count[0], count[1]);
+            for (int i = 0; ok && i < most; ++i) {
+                if (i < count[0]) ok = issue_o(s0, i);
+                if (ok && i + 1 < count[0]) ok = issue_s(s0);
+                if (ok && i < count[1]) ok = issue_o(s1, i);
+                if (ok && i + 1 < count[1]) ok = issue_s(s1);
+            }
         }
     } else if (warp == 2) {
         // ---------------------------------------------------------------- V rows behind the last candidate
@@ -273,17 +315,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         regs_inc<224>();
         const int s = (warp - 4) / 4, quarter = warp % 4, r = quarter * 32 + lane;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-        const uint32_t st = s_col[s] + lane_base, ot = o_col[s] + lane_base;
+        const uint32_t st = tmem + s * 128 + lane_base, ot = tmem + 256 + s * DP + lane_base;
         const int hr = r / p.tok, tr = t0 + (p.two_tiles ? s * p.tok : 0) + r % p.tok;
         const bool live = hr < n_heads && tr < u.n_q;
-        const int limit = live ? attend_limit(p.bv, u, tr, p.causal) : INT_MAX;
+        const int limit = live ? attend_limit(p.bv, u, tr, p.causal) : u.N;
+        // columns of tile t (of the request) that this row sees: one of these minus 128 t
+        const int in_cache = min(limit, u.c), in_chunk = limit - u.c + cache_tiles * kTileRows;
         const float growth = kGrowth / p.scale2;
         float m = -INFINITY, sum = 0.f;
         bool ok = true;
         for (int i = 0; i < count[s]; ++i) {
-            const KeyTile kt = key_tile(u, begin + tile_of(s, i));
-            const int nv = min(limit - kt.j0, kt.valid);   // columns that this row sees
-            if (!(ok = __all_sync(0xffffffffu, mbar_wait(&bar.s_full[s], i & 1, &abort_flag)))) break;
+            const int t = begin + tile_of(s, i), nv = (t < cache_tiles ? in_cache : in_chunk) - t * kTileRows;
+            if (!(ok = __all_sync(0xffffffffu, mbar_wait_now(&bar.s_full[s], i & 1, &abort_flag)))) break;
             tc_fence_after();
             uint32_t v[4][32];
 #pragma unroll
@@ -348,13 +391,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
             if (lane == 0) mbar_arrive(&bar.p_full[s]);
         }
         // ---- the row's result
-        if (count[s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.o_full[s], 0, &abort_flag));
+        if (count[s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait_now(&bar.o_full[s], 0, &abort_flag));
         tc_fence_after();
         const float m2 = m * p.scale2;   // the reference in base-2 logits (-inf: none of the row's keys)
         const bool shares = p.cluster > 1 || (!p.two_tiles && count[1] > 0);  // the result meets others in shared memory
         if (shares) {
             // the pages' place is free when the other stream's MMAs are complete, too
-            if (count[1 - s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(&bar.o_full[1 - s], 0, &abort_flag));
+            if (count[1 - s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait_now(&bar.o_full[1 - s], 0, &abort_flag));
             tc_fence_after();
             asm volatile("bar.sync 1, 256;" ::: "memory");
         }
