@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     auto frees = [&](int s, int t) { return !p.two_tiles || s == 1 || t >= count[1]; };
     constexpr int kStages = Lay::kStages;
 
-    if (warp < 4) regs_dec<56>();
+    if (warp < 4) regs_dec<104>();
     if (warp == 0) {
         // ---------------------------------------------------------------- producer
         if (lane == 0 && n_tiles > 0) {
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         }
     } else if (warp >= 4) {
         // ---------------------------------------------------------------- softmax
-        regs_inc<224>();
+        regs_inc<200>();
         const int s = (warp - 4) / 4, quarter = warp % 4, r = quarter * 32 + lane;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t st = tmem + s * 128 + lane_base, ot = tmem + 256 + s * DP + lane_base;
