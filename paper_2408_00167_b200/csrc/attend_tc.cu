@@ -28,7 +28,8 @@ using namespace tc;
 constexpr int kTcThreads = 384;      // 4 control warps, 2 x 4 softmax warps
 constexpr float kGrowth = 8.f;       // binary orders that a row's maximum may grow before O is scaled
 constexpr int kTileRows = 128;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 4;
+constexpr int kMaxParts = 2 * kMaxCluster;  // results of a row that meet in a cluster: its CTAs', of both streams where they share a row tile
 
 struct TcArgs {
     ModelView mv;
@@ -63,6 +64,9 @@ struct Barriers {
     uint64_t ragged[2], clean[2];  // the cache's, the chunk's last V tile: on its way, cleared behind its rows
 };
 
+// Where four columns of a row lie in a box: of 128 rows one behind the other, so that a warp's rows are read as one run.
+__device__ __forceinline__ int piece_at(int row, int piece) { return (piece * 128 + row) * 16; }
+
 // Where one row's result goes: the output and its log-sum-exp, or (unnormalised) the partial results of a split.
 struct Row {
     const TcArgs &p;
@@ -83,7 +87,7 @@ struct Row {
             return;
         }
         float lse;
-        inv = attend_finish(m, l, p.bv.self_lse, row, lse);
+        inv = attend_finish(m, l, p.bv.self_lse, row, lse);   // 0 for a row without keys
         if (notes && p.out.row_lse) p.out.row_lse[row] = lse;
     }
     __device__ __forceinline__ void put(int c, const float *y) {  // eight columns
@@ -111,9 +115,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     __shared__ int limit_s[2];
     uint8_t *smem = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     uint8_t *q_smem = smem, *ring = smem + 2 * Lay::kTile;
-    // a stream's result in the ring's place: [DP] columns of O, m, l, of 128 rows each
-    auto box = [&](int s) { return (float *)ring + s * (DP + 2) * 128; };
-    static_assert(2 * (DP + 2) * 128 * 4 <= Lay::kStages * Lay::kTile, "results take the ring's place");
+    // a stream's result in the ring's place: O of 128 rows, then (m, l) of each
+    auto box = [&](int s) { return ring + s * (DP * 512 + 1024); };
+    static_assert(2 * (DP * 512 + 1024) <= Lay::kStages * Lay::kTile, "results take the ring's place");
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     dependency_wait();
     const ModelView &mv = p.mv;
@@ -136,6 +140,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     // ---- set-up; how many candidates the rows of each stream see at most
     if (warp == 0) {
         if (lane == 0) {
+            prefetch_tensormap(&maps.q), prefetch_tensormap(&maps.ck), prefetch_tensormap(&maps.cv), prefetch_tensormap(&maps.hk), prefetch_tensormap(&maps.hv);
             mbar_init(&bar.q_full, 1);
             for (int i = 0; i < Lay::kStages; ++i) mbar_init(&bar.full[i], 1), mbar_init(&bar.empty[i], 1);
             for (int i = 0; i < 2; ++i)
@@ -176,6 +181,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     } else {
         count[0] = (n_tiles + 1) / 2, count[1] = n_tiles / 2;
     }
+    const bool gathers = p.cluster > 1 || (!p.two_tiles && count[1] > 0);   // rows' results meet others in shared memory
     auto tile_of = [&](int s, int i) { return p.two_tiles ? i : 2 * i + s; };  // in the split
     // the last stream to use a tile frees it
     auto frees = [&](int s, int t) { return !p.two_tiles || s == 1 || t >= count[1]; };
@@ -394,114 +400,114 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         if (count[s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait_now(&bar.o_full[s], 0, &abort_flag));
         tc_fence_after();
         const float m2 = m * p.scale2;   // the reference in base-2 logits (-inf: none of the row's keys)
-        const bool shares = p.cluster > 1 || (!p.two_tiles && count[1] > 0);  // the result meets others in shared memory
-        if (shares) {
+        if (!gathers) {
+            Row row(p, u, l, h0 + hr, tr, live && (p.two_tiles || s == 0), split);
+            row.finish(m2, sum);
+#pragma unroll 1
+            for (int c = 0; c < mv.d; c += 16) {
+                uint32_t o[16];
+                float y[16];
+                if (count[s] > 0) {
+                    tmem_ld_issue(ot + c, o);
+                    tmem_ld_wait(o);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) y[e] = count[s] > 0 ? __uint_as_float(o[e]) : 0.f;
+                row.put(c, y);
+                row.put(c + 8, y + 8);
+                __syncwarp();
+            }
+        } else {
             // the pages' place is free when the other stream's MMAs are complete, too
             if (count[1 - s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait_now(&bar.o_full[1 - s], 0, &abort_flag));
             tc_fence_after();
             asm volatile("bar.sync 1, 256;" ::: "memory");
-        }
-        float scale_o = 1.f, total = sum, ref = m2, other = 0.f;
-        float *mine = box(p.two_tiles ? s : 0);
-        if (!p.two_tiles && count[1] > 0) {
-            if (s == 1) {
+            if (count[s] > 0) {
 #pragma unroll 1
-                for (int c = 0; c < DP / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld_issue(ot + c * 32, o);
+                for (int c = 0; c < DP; c += 16) {
+                    uint32_t o[16];
+                    tmem_ld_issue(ot + c, o);
                     tmem_ld_wait(o);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * 128 + r] = __uint_as_float(o[e]);
+                    for (int e = 0; e < 16; e += 4) *(uint4 *)(box(s) + piece_at(r, (c + e) / 4)) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 }
-                mine[DP * 128 + r] = m2;
-                mine[(DP + 1) * 128 + r] = sum;
             }
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (s == 0) {
-                const float mo = mine[DP * 128 + r], lo = mine[(DP + 1) * 128 + r];
-                ref = fmaxf(sum == 0.f ? -INFINITY : m2, lo == 0.f ? -INFINITY : mo);
-                const float base = ref == -INFINITY ? 0.f : ref;
-                scale_o = sum == 0.f ? 0.f : exp2f(m2 - base);
-                other = lo == 0.f ? 0.f : exp2f(mo - base);
-                total = sum * scale_o + lo * other;
-            }
+            *(float2 *)(box(s) + DP * 512 + r * 8) = make_float2(m2, count[s] > 0 ? sum : 0.f);
         }
-        const bool holds = p.two_tiles || s == 0;   // the row's result is in these warps
-        Row row(p, u, l, h0 + hr, tr, live && holds, split / p.cluster);
-        if (holds && p.cluster == 1) row.finish(ref, total);
-#pragma unroll 1
-        for (int c = 0; c < (p.cluster > 1 ? DP : mv.d) / 32 && holds; ++c) {
-            uint32_t o[32];
-            if (count[s] > 0) {
-                tmem_ld_issue(ot + c * 32, o);
-                tmem_ld_wait(o);
-            }
-            float y[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                y[e] = count[s] > 0 && sum != 0.f ? __uint_as_float(o[e]) * scale_o : 0.f;
-                if (other != 0.f) y[e] = fmaf(mine[(c * 32 + e) * 128 + r], other, y[e]);
-            }
-            if (p.cluster > 1) {
-#pragma unroll
-                for (int e = 0; e < 32; ++e) mine[(c * 32 + e) * 128 + r] = y[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 32; e += 8) row.put(c * 32 + e, &y[e]);
-            }
-            __syncwarp();
-        }
-        if (holds && p.cluster > 1) mine[DP * 128 + r] = ref, mine[(DP + 1) * 128 + r] = total;
         tc_fence_before();
     }
-    if (p.cluster > 1) {
-        // ---- the splits of the cluster: every CTA adds all of them for some columns, from their shared memory
+    if (gathers) {
+        // ---- the streams and the CTAs that worked on the same rows: every CTA adds all of them for some columns
         __syncwarp();
-        cluster_arrive();
-        cluster_wait();
-        if (warp >= 4) {
-            const int rank = split % p.cluster, boxes = p.two_tiles ? 2 : 1;
-            for (int task = warp - 4;; task += 8) {
-                const int x = task / 4 % boxes, c0 = (rank + task / 4 / boxes * p.cluster) * 8, r = task % 4 * 32 + lane;
-                if (c0 >= mv.d) break;
-                const uint32_t at = smem_u32(box(x)) + r * 4;
-                const int hr = r / p.tok, tr = t0 + x * p.tok + r % p.tok;
-                Row row(p, u, l, h0 + hr, tr, hr < n_heads && tr < u.n_q, split / p.cluster);
-                float m[kMaxCluster], f[kMaxCluster], ref = -INFINITY, total = 0.f, y[8];
-#pragma unroll
-                for (int j = 0; j < kMaxCluster; ++j) {
-                    m[j] = -INFINITY, f[j] = 0.f;
-                    if (j < p.cluster) {
-                        m[j] = ld_remote_f32(map_to_rank(at + DP * 512, j));
-                        f[j] = ld_remote_f32(map_to_rank(at + (DP + 1) * 512, j));
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < kMaxCluster; ++j)
-                    if (f[j] != 0.f) ref = fmaxf(ref, m[j]);
-                const float base = ref == -INFINITY ? 0.f : ref;
-#pragma unroll
-                for (int j = 0; j < kMaxCluster; ++j) {
-                    const float g = f[j] == 0.f ? 0.f : ex2(m[j] - base);
-                    total = fmaf(f[j], g, total);
-                    f[j] = g;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = 0.f;
-#pragma unroll
-                for (int j = 0; j < kMaxCluster; ++j)
-                    if (j < p.cluster) {
-                        const uint32_t from = map_to_rank(at + c0 * 512, j);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] = fmaf(ld_remote_f32(from + e * 512), f[j], y[e]);
-                    }
-                row.finish(ref, total, c0 == 0);
-                row.put(c0, y);
-            }
+        if (p.cluster > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else if (warp >= 4) {
+            asm volatile("bar.sync 1, 256;" ::: "memory");
         }
-        __syncwarp();
-        cluster_arrive();
-        cluster_wait();   // nobody reads this CTA's shared memory any more
+        if (warp >= 4) {
+            const int rank = split % p.cluster, r = warp % 4 * 32 + lane;
+            const int sets = p.two_tiles ? 2 : 1, parts = p.two_tiles ? p.cluster : 2 * p.cluster;
+            const uint32_t box0 = smem_u32(box(0)), box1 = smem_u32(box(1));
+            auto add = [&](auto remote) {
+                constexpr bool kRemote = decltype(remote)::value == 1;
+                for (int set = 0; set < sets; ++set) {
+                    const int hr = r / p.tok, tr = t0 + set * p.tok + r % p.tok;
+                    Row row(p, u, l, h0 + hr, tr, hr < n_heads && tr < u.n_q, split / p.cluster);
+                    auto part_at = [&](int j) {
+                        const uint32_t at = (p.two_tiles ? set : j % 2) ? box1 : box0;
+                        return kRemote ? map_to_rank(at, p.two_tiles ? j : j / 2) : at;
+                    };
+                    float m[kMaxParts], f[kMaxParts], ref = -INFINITY, total = 0.f;
+#pragma unroll
+                    for (int j = 0; j < kMaxParts; ++j) {
+                        m[j] = -INFINITY, f[j] = 0.f;
+                        if (j < parts) {
+                            const uint32_t at = part_at(j) + DP * 512 + r * 8;
+                            const float2 ml = kRemote ? ld_remote(at) : lds64(at);
+                            m[j] = ml.x, f[j] = ml.y;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < kMaxParts; ++j)
+                        if (f[j] != 0.f) ref = fmaxf(ref, m[j]);
+                    const float base = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+                    for (int j = 0; j < kMaxParts; ++j) {
+                        const float g = f[j] == 0.f ? 0.f : ex2(m[j] - base);
+                        total = fmaf(f[j], g, total);
+                        f[j] = g;
+                    }
+                    row.finish(ref, total, rank == 0 && warp < 8);
+#pragma unroll 1
+                    for (int c = (rank + (warp - 4) / 4 * p.cluster) * 8; c < mv.d; c += 16 * p.cluster) {
+                        float4 a[kMaxParts][2];
+#pragma unroll
+                        for (int j = 0; j < kMaxParts; ++j)
+                            if (j < parts) {
+                                const uint32_t at = part_at(j) + piece_at(r, c / 4);
+                                a[j][0] = kRemote ? ld_remote_f32x4(at) : lds128(at);
+                                a[j][1] = kRemote ? ld_remote_f32x4(at + 2048) : lds128(at + 2048);
+                            }
+                        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int j = 0; j < kMaxParts; ++j)
+                            if (f[j] != 0.f) {  // .. and was written
+                                const float g = f[j];
+                                y[0] = fmaf(a[j][0].x, g, y[0]), y[1] = fmaf(a[j][0].y, g, y[1]), y[2] = fmaf(a[j][0].z, g, y[2]), y[3] = fmaf(a[j][0].w, g, y[3]);
+                                y[4] = fmaf(a[j][1].x, g, y[4]), y[5] = fmaf(a[j][1].y, g, y[5]), y[6] = fmaf(a[j][1].z, g, y[6]), y[7] = fmaf(a[j][1].w, g, y[7]);
+                            }
+                        row.put(c, y);
+                    }
+                }
+            };
+            if (p.cluster > 1) add(Stream<1>{}); else add(Stream<0>{});
+        }
+        if (p.cluster > 1) {
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();   // nobody reads this CTA's shared memory any more
+        }
     }
     __syncthreads();
     if (warp == 1) {
@@ -539,25 +545,26 @@ bool make_q_map(CUtensorMap *map, const TensorView &t, int d, int64_t tokens, in
 }
 
 // Key splits of a call of `units` CTAs with `tiles` key tiles at most: first the CTAs of a cluster, then, for few rows and long
-// contexts, several clusters whose results merge_splits adds.  A key tile takes a CTA about a microsecond (half of that with two
-// streams on one row tile), the cluster's sum about three, a merge of clusters about five.
+// contexts, several clusters whose results merge_splits adds.  In microseconds, measured with 512 rows a KV head on 8 of them: a key tile
+// takes a CTA 1.8 (two row tiles) or 0.85 (two streams on one), the sum in a cluster of c CTAs about 8 or 1 + 0.8 c, a merge of
+// clusters about 5 (128 prompt rows over 2176 keys: 26 without, 20 with clusters of two, 19 of four; 32 rows over 8224: 66, 41,
+// 28, and 22 as four clusters of four).
 void choose_splits(int sms, int64_t units, int tiles, int two_tiles, size_t room, int &cluster, int &splits) {
     cluster = splits = 1;
-    const double tile_us = two_tiles ? 1.0 : 0.5;
+    const double tile_us = two_tiles ? 1.8 : 0.85;
+    const int64_t slots = (int64_t)(sms / 18) * 16;   // SMs of GPCs of 16 to 18, in whole clusters
     auto waves = [&](int64_t ctas) { return (double)((ctas + sms - 1) / sms); };
     double best = waves(units) * tiles * tile_us;
-    for (int c = 2; c <= kMaxCluster; ++c) {
-        // clusters of c CTAs that a device of GPCs of 16 to 18 SMs holds at a time
-        const int64_t at_once = (int64_t)(sms / 18) * (16 / c) * c;
-        if (units * c > at_once || tiles < 2 * c) break;
-        const double t = (double)((tiles + c - 1) / c) * tile_us + 3.0;
+    for (int c = 2; c <= kMaxCluster; c *= 2) {
+        if (units * c > slots || tiles < 2 * c) break;
+        const double t = (double)((tiles + c - 1) / c) * tile_us + (two_tiles ? 8.0 : 1.0 + 0.8 * c);
         if (t < best) best = t, cluster = splits = c;
     }
     if (cluster == kMaxCluster) {
         for (int g = 2; g <= kAttendMaxSplits && (size_t)g <= room; ++g) {
             const int c = cluster * g;
-            if (units * c > (int64_t)(sms / 18) * 16 || tiles < 2 * c) break;
-            const double t = (double)((tiles + c - 1) / c) * tile_us + 8.0;
+            if (units * c > slots || tiles < 2 * c) break;
+            const double t = (double)((tiles + c - 1) / c) * tile_us + (two_tiles ? 8.0 : 1.0 + 0.8 * cluster) + 5.0;
             if (t < best) best = t, splits = c;
         }
     }
@@ -575,7 +582,9 @@ cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorVi
     p.heads = mv.g < kTileRows ? mv.g : kTileRows;
     p.tok = kTileRows / p.heads;
     p.chunks = (mv.g + p.heads - 1) / p.heads;
-    p.two_tiles = bv.max_q > p.tok;
+    // Two row tiles to a CTA, unless that leaves more than half of the SMs without one.
+    const int64_t units = (int64_t)mv.L * mv.Hkv * p.chunks, one_tile = units * bv.batch * ((bv.max_q + p.tok - 1) / p.tok);
+    p.two_tiles = bv.max_q > p.tok && 2 * one_tile > ctx.sm_count;
     const int per_cta = p.two_tiles ? 2 * p.tok : p.tok;
     p.row_tiles = (bv.max_q + per_cta - 1) / per_cta;
     Maps maps;
@@ -590,7 +599,6 @@ cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorVi
         return cudaErrorNotSupported;
     if (!cache) maps.ck = maps.cv = maps.q;
     if (!chunk) maps.hk = maps.hv = maps.q;
-    const int64_t units = (int64_t)mv.L * mv.Hkv * p.chunks;
     const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
     const int key_tiles = (bv.max_cache + kTileRows - 1) / kTileRows + (bv.max_chunk + kTileRows - 1) / kTileRows;
     choose_splits(ctx.sm_count, units * p.row_tiles * bv.batch, key_tiles, p.two_tiles, partial_rows / (rows > 0 ? rows : 1), p.cluster, p.out.splits);

@@ -126,9 +126,9 @@ __device__ __forceinline__ float2 ld_remote(uint32_t mapped) {
     asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(mapped) : "memory");
     return v;
 }
-__device__ __forceinline__ float ld_remote_f32(uint32_t mapped) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(mapped) : "memory");
+__device__ __forceinline__ float4 ld_remote_f32x4(uint32_t mapped) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(mapped) : "memory");
     return v;
 }
 // mbar_wait for a barrier on which other CTAs of the cluster arrive after writing what the waiter will read.
