@@ -481,22 +481,26 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     row.finish(ref, total, rank == 0 && warp < 8);
 #pragma unroll 1
                     for (int c = (rank + (warp - 4) / 4 * p.cluster) * 8; c < mv.d; c += 16 * p.cluster) {
-                        float4 a[kMaxParts][2];
-#pragma unroll
-                        for (int j = 0; j < kMaxParts; ++j)
-                            if (j < parts) {
-                                const uint32_t at = part_at(j) + piece_at(r, c / 4);
-                                a[j][0] = kRemote ? ld_remote_f32x4(at) : lds128(at);
-                                a[j][1] = kRemote ? ld_remote_f32x4(at + 2048) : lds128(at + 2048);
-                            }
                         float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int j = 0; j < kMaxParts; ++j)
-                            if (f[j] != 0.f) {  // .. and was written
-                                const float g = f[j];
-                                y[0] = fmaf(a[j][0].x, g, y[0]), y[1] = fmaf(a[j][0].y, g, y[1]), y[2] = fmaf(a[j][0].z, g, y[2]), y[3] = fmaf(a[j][0].w, g, y[3]);
-                                y[4] = fmaf(a[j][1].x, g, y[4]), y[5] = fmaf(a[j][1].y, g, y[5]), y[6] = fmaf(a[j][1].z, g, y[6]), y[7] = fmaf(a[j][1].w, g, y[7]);
-                            }
+                        for (int j0 = 0; j0 < kMaxParts; j0 += 4) {
+                            if (j0 >= parts) break;
+                            float4 a[4][2];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (j0 + j < parts) {
+                                    const uint32_t at = part_at(j0 + j) + piece_at(r, c / 4);
+                                    a[j][0] = kRemote ? ld_remote_f32x4(at) : lds128(at);
+                                    a[j][1] = kRemote ? ld_remote_f32x4(at + 2048) : lds128(at + 2048);
+                                }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (f[j0 + j] != 0.f) {  // .. and was written
+                                    const float g = f[j0 + j];
+                                    y[0] = fmaf(a[j][0].x, g, y[0]), y[1] = fmaf(a[j][0].y, g, y[1]), y[2] = fmaf(a[j][0].z, g, y[2]), y[3] = fmaf(a[j][0].w, g, y[3]);
+                                    y[4] = fmaf(a[j][1].x, g, y[4]), y[5] = fmaf(a[j][1].y, g, y[5]), y[6] = fmaf(a[j][1].z, g, y[6]), y[7] = fmaf(a[j][1].w, g, y[7]);
+                                }
+                        }
                         row.put(c, y);
                     }
                 }
