@@ -1,0 +1,277 @@
+"""Refusals and host arithmetic of finch_rotate, finch_attend and the paged cache; no GPU (a validation-only context)."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from paper_2408_00167_b200 import binding as fb
+from paper_2408_00167_b200 import build as fbuild
+
+OK, INVALID, UNSUPPORTED, LAYOUT, SMALL = (fb.FINCH_OK, fb.FINCH_ERR_INVALID_ARG, fb.FINCH_ERR_UNSUPPORTED, fb.FINCH_ERR_BAD_LAYOUT,
+                                           fb.FINCH_ERR_WORKSPACE_TOO_SMALL)
+BASE = 0x7000_0000_0000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    fbuild.build()
+    return fb.load()
+
+
+@pytest.fixture()
+def ctx(lib):
+    c = fb.finch_ctx_create(2, 8, 2, 64, fb.FINCH_BF16, max_batch=4, max_prompt=64, max_candidates=1024, device=-1)
+    yield c
+    fb.finch_ctx_destroy(c)
+
+
+def tensor(slot, tokens, heads, d=64, shift=0, token_major=False, stride_tok=None):
+    """Addresses only: validation never follows them."""
+    at = BASE + 0x1000_0000 * (slot + 1) + shift
+    if token_major:
+        return fb.finch_tensor(at, tokens * heads * d, d, heads * d)
+    st = d if stride_tok is None else stride_tok
+    return fb.finch_tensor(at, heads * tokens * st, tokens * st, st)
+
+
+NULL = fb.finch_tensor(None, 0, 0, 0)
+
+
+def rope(rotary=64, pairing=0, magnitude=1.0):
+    return fb.finch_rope_init(rotary, np.ones(rotary // 2), pairing, magnitude)
+
+
+def test_frequencies_of_every_scaling(lib):
+    """Against the formulas, and what they are for: the ends of the spectrum that a scaling keeps or divides."""
+    plain = fb.finch_rope_frequencies(64, 10000.0)
+    np.testing.assert_allclose(plain, 10000.0 ** (-2 * np.arange(32) / 64), rtol=1e-14)
+    np.testing.assert_allclose(fb.finch_rope_frequencies(64, 10000.0, fb.FINCH_ROPE_LINEAR, 4.0), plain / 4, rtol=1e-14)
+    base = fb.finch_rope_frequencies(64, 10000.0, fb.FINCH_ROPE_BASE, 4.0)
+    assert base[0] == plain[0]
+    np.testing.assert_allclose(base[-1], plain[-1] / 4, rtol=1e-12)      # the slowest pair is stretched by the whole factor
+    parts = fb.finch_rope_frequencies(64, 10000.0, fb.FINCH_ROPE_PARTS, 4.0, original=4096, low=1, high=4)
+    turns = 4096 * plain / (2 * math.pi)
+    np.testing.assert_array_equal(parts[turns >= 4], plain[turns >= 4])
+    np.testing.assert_allclose(parts[turns <= 1], plain[turns <= 1] / 4, rtol=1e-14)
+    mid = (turns > 1) & (turns < 4)
+    assert mid.any() and np.all(parts[mid] < plain[mid]) and np.all(parts[mid] > plain[mid] / 4)
+
+
+@pytest.mark.parametrize("args", [(0, 1e4), (63, 1e4), (258, 1e4), (64, 0.5), (64, math.nan), (64, math.inf), (64, 1e4, 4), (64, 1e4, -1),
+                                  (64, 1e4, 1, 0.5), (64, 1e4, 2, math.nan), (2, 1e4, 2, 2.0), (64, 1e4, 3, 2.0, 0.0),
+                                  (64, 1e4, 3, 2.0, 8192.0, 4.0, 4.0), (64, 1e4, 3, 2.0, 8192.0, -1.0, 4.0)])
+def test_frequencies_refuse(lib, args):
+    with pytest.raises(fb.FinchError) as e:
+        fb.finch_rope_frequencies(*args)
+    assert e.value.status == INVALID
+
+
+@pytest.mark.parametrize("rotary,freq,pairing,magnitude,status", [
+    (64, np.ones(32), 2, 1.0, INVALID), (64, np.ones(32), 0, math.nan, INVALID), (64, np.full(32, math.nan), 0, 1.0, INVALID),
+    (64, np.full(32, 2.5), 0, 1.0, INVALID), (24, np.ones(12), 0, 1.0, UNSUPPORTED)])
+def test_rope_init_refuses(lib, rotary, freq, pairing, magnitude, status):
+    with pytest.raises(fb.FinchError) as e:
+        fb.finch_rope_init(rotary, freq, pairing, magnitude)
+    assert e.value.status == status
+    with pytest.raises(ValueError):
+        fb.finch_rope_init(64, np.ones(31))
+
+
+def test_rotate_refuses(lib, ctx):
+    r = rope()
+
+    def call(q=None, k=None, oq=None, ok=None, tokens=10, pos=BASE, rp=r, qw=None, kw=None, eps=1e-6):
+        q, k = q or tensor(0, 10, 8), k or tensor(1, 10, 2)
+        oq, ok = oq or tensor(2, 10, 8), ok or tensor(3, 10, 2)
+        return lib.finch_rotate(ctx, C.addressof(q), C.addressof(k), tokens, pos, C.addressof(rp) if rp else None, qw, kw, eps,
+                                C.addressof(oq), C.addressof(ok), None)
+    assert call() == UNSUPPORTED                                  # valid: stops at the launch
+    assert call(oq=tensor(0, 10, 8), ok=tensor(1, 10, 2)) == UNSUPPORTED      # in place
+    assert call(k=NULL, ok=NULL) == UNSUPPORTED                   # queries alone
+    assert call(rp=None, qw=BASE, pos=None) == UNSUPPORTED        # norm alone
+    assert call(tokens=0, q=NULL, k=NULL, oq=NULL, ok=NULL) == UNSUPPORTED
+    assert call(tokens=-1) == INVALID
+    assert call(pos=None) == INVALID
+    assert call(rp=None) == INVALID                               # nothing to do
+    assert call(k=NULL) == INVALID                                # an output without its tensor
+    assert call(q=NULL, k=NULL, oq=NULL, ok=NULL) == INVALID
+    assert call(qw=BASE, eps=-1.0) == INVALID
+    assert call(qw=BASE, eps=math.nan) == INVALID
+    assert call(qw=BASE + 8) == LAYOUT
+    assert call(q=tensor(0, 10, 8, shift=8)) == LAYOUT
+    assert call(q=tensor(0, 10, 8, stride_tok=60)) == LAYOUT
+    assert call(oq=tensor(0, 10, 8, shift=128)) == INVALID        # rows of the output over other rows of the input
+    assert call(ok=tensor(0, 10, 2)) == INVALID
+    assert call(oq=tensor(3, 10, 8)) == INVALID                   # the outputs over one another
+    wide = rope(128)
+    assert call(rp=wide) == INVALID                               # wider than a head
+    bad = rope()
+    bad.rotary_dim = 40
+    assert call(rp=bad) == UNSUPPORTED
+    # queries and keys side by side in one row of a fused projection, in place
+    buf = lambda shift: fb.finch_tensor(BASE + shift * 2, 10 * 12 * 64, 64, 12 * 64)
+    assert call(q=buf(0), k=buf(8 * 64), oq=buf(0), ok=buf(8 * 64)) == UNSUPPORTED
+    assert call(q=buf(0), k=buf(7 * 64), oq=buf(0), ok=buf(7 * 64)) == INVALID
+    assert lib.finch_rotate(None, None, None, 0, None, None, None, None, 0.0, None, None, None) == INVALID
+
+
+def _batch(B=2, q=40, m=90, c=70, max_q=30, max_m=50, max_c=40, row_norm=0):
+    return fb.finch_batch(B, BASE, BASE, BASE, BASE, BASE, q, m, c, max_q, max_c, max_m, 0, None, None, row_norm)
+
+
+def test_attend_refuses(lib, ctx):
+    def call(b=None, causal=1, out=None, ws=BASE, ws_bytes=1 << 40, **other):
+        b = b or _batch()
+        t = dict(q=tensor(0, b.total_q, 8), ck=tensor(1, b.total_cache, 2), cv=tensor(2, b.total_cache, 2), hk=tensor(3, b.total_chunk, 2),
+                 hv=tensor(4, b.total_chunk, 2))
+        t.update(other)
+        out = out or tensor(5, b.total_q, 8)
+        return lib.finch_attend(ctx, *(C.addressof(t[n]) for n in ("q", "ck", "cv", "hk", "hv")), C.addressof(b), causal, C.addressof(out), None,
+                                ws, ws_bytes, None)
+    assert call() == UNSUPPORTED
+    assert call(_batch(c=0, max_c=0), ck=NULL, cv=NULL) == UNSUPPORTED            # no cache
+    assert call(_batch(m=0, max_m=0), hk=NULL, hv=NULL) == UNSUPPORTED            # no chunk
+    assert call(q=tensor(0, 40, 8, token_major=True), out=tensor(5, 40, 8, token_major=True)) == UNSUPPORTED
+    assert call(causal=2) == INVALID
+    assert call(_batch(row_norm=1)) == INVALID
+    assert call(q=NULL) == INVALID
+    assert call(cv=NULL) == INVALID
+    assert call(_batch(max_q=65, q=100)) == INVALID                               # beyond the context's prompt
+    assert call(_batch(max_c=1000, c=1000)) == INVALID
+    assert call(_batch(B=5)) == INVALID
+    assert call(hv=tensor(4, 90, 2, shift=4)) == LAYOUT
+    assert call(out=tensor(0, 40, 8)) == INVALID                                  # over the queries
+    assert call(out=tensor(4, 40, 8, shift=-64 * 2 * 5)) == INVALID               # over the chunk's values
+    assert call(ws=None) == INVALID
+    assert call(ws=BASE + 8) == LAYOUT
+    need = C.c_size_t()
+    b = _batch()
+    assert lib.finch_attend_workspace_bytes(ctx, C.addressof(b), C.addressof(need)) == OK
+    assert call(ws_bytes=need.value - 1) == SMALL and call(ws_bytes=need.value) == UNSUPPORTED
+    assert lib.finch_attend_workspace_bytes(ctx, C.addressof(b), None) == INVALID
+    assert lib.finch_attend_workspace_bytes(ctx, None, C.addressof(need)) == INVALID
+
+
+def test_attend_workspace_of_the_most_rows_serves_every_call(lib):
+    for L, Hq, Hkv, d in ((1, 32, 8, 128), (32, 32, 8, 128), (1, 64, 1, 256), (2, 3, 3, 32)):
+        c = fb.finch_ctx_create(L, Hq, Hkv, d, fb.FINCH_BF16, max_batch=9, max_prompt=5000, max_candidates=100000, device=-1)
+        room = 0
+        for rows in (1, 2, 31, 32, 33, 100, 1000, 5000):
+            b = _batch(B=1, q=rows, max_q=rows)
+            need = C.c_size_t()
+            assert lib.finch_attend_workspace_bytes(c, C.addressof(b), C.addressof(need)) == OK
+            assert need.value >= room and need.value % 256 == 0
+            room = need.value
+        fb.finch_ctx_destroy(c)
+
+
+def _pages(**kw):
+    base = dict(k=BASE, v=BASE + (1 << 30), k_scale=BASE, v_scale=BASE, open_k=BASE, open_v=BASE, table=BASE, open_slot=None, n_pages=40,
+                table_width=8, n_open=4)
+    base.update(kw)
+    return fb.finch_pages(*base.values())
+
+
+def _paged(B=2, q=4, n=100, max_q=2, max_n=60, max_len=400, q_off=BASE, new_off=BASE, length=BASE):
+    return fb.finch_paged_batch(B, q_off, new_off, length, q, n, max_q, max_n, max_len)
+
+
+def _append(lib, ctx, pages=None, batch=None, k=None, v=None, r=None, out_len=BASE + 4096):
+    pages, batch = pages or _pages(), batch or _paged()
+    k, v = k or tensor(0, max(batch.total_new, 1), 2), v or tensor(1, max(batch.total_new, 1), 2)
+    return lib.finch_pages_append(ctx, C.addressof(pages), C.addressof(batch), C.addressof(k), C.addressof(v), C.addressof(r) if r else None,
+                                  None, out_len, None)
+
+
+def _decode(lib, ctx, pages=None, batch=None, q=None, out=None, ws=BASE, ws_bytes=1 << 40):
+    pages, batch = pages or _pages(), batch or _paged()
+    q, out = q or tensor(0, max(batch.total_q, 1), 8), out or tensor(1, max(batch.total_q, 1), 8)
+    return lib.finch_pages_attend(ctx, C.addressof(pages), C.addressof(batch), C.addressof(q), C.addressof(out), None, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("call", [_append, _decode])
+def test_paged_calls_refuse(lib, ctx, call):
+    assert call(lib, ctx) == UNSUPPORTED
+    assert call(lib, ctx, batch=_paged(B=0, q=0, n=0, max_q=0, max_n=0)) == UNSUPPORTED
+    assert call(lib, ctx, _pages(k=None, v=None, k_scale=None, v_scale=None, table=None, n_pages=0, table_width=0),
+                _paged(max_len=3, max_n=60, n=60)) == UNSUPPORTED                 # no page is full: only open rows
+    for bad in (dict(open_k=None), dict(open_v=None), dict(n_open=0), dict(n_open=1), dict(n_pages=0), dict(n_pages=-1), dict(table=None),
+                dict(table_width=3), dict(k=None), dict(v=None), dict(k_scale=None), dict(v_scale=None)):
+        assert call(lib, ctx, _pages(**bad)) == INVALID, bad
+    assert call(lib, ctx, _pages(open_slot=BASE, n_open=1)) == UNSUPPORTED        # slots of their own
+    for bad in (dict(k=BASE + 4), dict(v=BASE + 8), dict(open_k=BASE + 2), dict(open_v=BASE + 8)):
+        assert call(lib, ctx, _pages(**bad)) == LAYOUT, bad
+    for bad in (dict(B=-1), dict(B=5), dict(max_len=-1), dict(max_len=1025), dict(length=None)):
+        assert call(lib, ctx, batch=_paged(**bad)) == INVALID, bad
+
+
+def test_append_refuses(lib, ctx):
+    assert _append(lib, ctx, batch=_paged(new_off=None)) == INVALID
+    assert _append(lib, ctx, batch=_paged(q_off=None)) == UNSUPPORTED             # not read here
+    assert _append(lib, ctx, batch=_paged(max_n=101)) == INVALID
+    assert _append(lib, ctx, batch=_paged(n=-1)) == INVALID
+    assert _append(lib, ctx, batch=_paged(max_len=1000)) == INVALID               # 1060 tokens of 1024
+    assert _append(lib, ctx, k=NULL) == INVALID
+    assert _append(lib, ctx, k=tensor(0, 100, 2, shift=8)) == LAYOUT
+    assert _append(lib, ctx, r=rope(128)) == INVALID
+    assert _append(lib, ctx, out_len=None) == UNSUPPORTED
+    assert _append(lib, ctx, out_len=BASE) == INVALID                             # in place of the lengths
+    assert _append(lib, ctx, out_len=BASE + 4) == INVALID
+    assert _append(lib, ctx, out_len=BASE + 8) == UNSUPPORTED
+
+
+def test_paged_attention_refuses(lib, ctx):
+    assert _decode(lib, ctx, batch=_paged(q_off=None)) == INVALID
+    assert _decode(lib, ctx, batch=_paged(new_off=None)) == UNSUPPORTED
+    assert _decode(lib, ctx, batch=_paged(max_q=5)) == INVALID
+    assert _decode(lib, ctx, batch=_paged(q=200, max_q=65)) == INVALID
+    assert _decode(lib, ctx, q=NULL) == INVALID
+    assert _decode(lib, ctx, out=tensor(0, 4, 8)) == INVALID
+    assert _decode(lib, ctx, ws=None) == INVALID
+    assert _decode(lib, ctx, ws=BASE + 4) == LAYOUT
+    b, need = _paged(), C.c_size_t()
+    assert lib.finch_pages_workspace_bytes(ctx, C.addressof(b), C.addressof(need)) == OK
+    assert _decode(lib, ctx, ws_bytes=need.value - 1) == SMALL and _decode(lib, ctx, ws_bytes=need.value) == UNSUPPORTED
+    assert lib.finch_pages_workspace_bytes(None, C.addressof(b), C.addressof(need)) == INVALID
+    assert lib.finch_pages_workspace_bytes(ctx, C.addressof(b), None) == INVALID
+
+
+def test_the_binding_refuses_other_types_shapes_and_devices(lib, ctx):
+    """What the C call cannot see: a tensor of another dtype or shape.  Nothing is enqueued (the tensors are the CPU's)."""
+    import torch
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    q, k = bf(2, 8, 5, 64), bf(2, 2, 5, 64)
+    pos = torch.zeros(5, dtype=torch.int32)
+    r = rope()
+    for kw in (dict(k=k.float()), dict(k=bf(2, 2, 6, 64)), dict(out_q=bf(2, 8, 4, 64)), dict(pos=pos.long()), dict(pos=pos[:4]),
+               dict(q_weight=bf(64)), dict(q_weight=torch.zeros(2, 64)), dict(out_k=None), dict(q=q.transpose(2, 3))):
+        a = dict(q=q, k=k, pos=pos, out_q=torch.empty_like(q), out_k=torch.empty_like(k), rope=r)
+        a.update(kw)
+        with pytest.raises(ValueError):
+            fb.finch_rotate(ctx, **a)
+    batch = fb.make_batch([0, 5], [0, 5], [0, 0], [0], [0], device="cpu")
+    e, lse, ws = bf(2, 2, 0, 64), torch.zeros((2, 8, 5)), torch.zeros(1 << 20, dtype=torch.uint8)
+    for kw in (dict(chunk_v=k.float()), dict(out=bf(2, 8, 6, 64)), dict(row_lse=lse.double()), dict(row_lse=lse[:, :4])):
+        a = dict(q=q, cache_k=e, cache_v=e, chunk_k=k, chunk_v=k, batch=batch, out=torch.empty_like(q), row_lse=lse, ws=ws)
+        a.update(kw)
+        with pytest.raises(ValueError):
+            fb.finch_attend(ctx, **a)
+    pool = lambda dtype=torch.uint8: torch.zeros((2, 3, 2, 64, 64), dtype=dtype)
+    good = dict(k=pool(), v=pool(), k_scale=torch.zeros((2, 3, 2)), v_scale=torch.zeros((2, 3, 2)), open_k=bf(2, 1, 2, 64, 64), open_v=bf(2, 1, 2, 64, 64),
+                table=torch.zeros((1, 3), dtype=torch.int32))
+    for kw in (dict(v=pool(torch.int8)), dict(k_scale=torch.zeros((2, 2, 2))), dict(open_v=torch.zeros((2, 1, 2, 64, 64))),
+               dict(table=torch.zeros((1, 3))), dict(open_slot=torch.zeros(2, dtype=torch.int32)), dict(k=pool()[:, :, :, :32])):
+        with pytest.raises(ValueError):
+            fb.make_pages(**{**good, **kw})
+    pages, paged = fb.make_pages(**good), fb.make_paged_batch([10], q_off=[0, 5], new_off=[0, 5], device="cpu")
+    with pytest.raises(ValueError):
+        fb.finch_pages_append(ctx, pages, paged, k.float(), k)
+    with pytest.raises(ValueError):
+        fb.finch_pages_append(ctx, pages, paged, k, k, out_len=torch.zeros(1))
+    with pytest.raises(ValueError):
+        fb.finch_pages_attend(ctx, pages, paged, q, bf(2, 8, 4, 64), ws=ws)
+    with pytest.raises(ValueError):
+        fb.make_paged_batch([10], new_off=[0, 5], len_tensor=torch.zeros(1), device="cpu")
+
+
