@@ -60,7 +60,7 @@ struct Layout {
 };
 
 struct Barriers {
-    uint64_t q_full, full[8], empty[8], s_full[2], p_full[2], o_full[2];
+    uint64_t q_full[2], full[8], empty[8], s_full[2], p_full[2], o_full[2];
     uint64_t ragged[2], clean[2];  // the cache's, the chunk's last V tile: on its way, cleared behind its rows
 };
 
@@ -141,10 +141,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     if (warp == 0) {
         if (lane == 0) {
             prefetch_tensormap(&maps.q), prefetch_tensormap(&maps.ck), prefetch_tensormap(&maps.cv), prefetch_tensormap(&maps.hk), prefetch_tensormap(&maps.hv);
-            mbar_init(&bar.q_full, 1);
             for (int i = 0; i < Lay::kStages; ++i) mbar_init(&bar.full[i], 1), mbar_init(&bar.empty[i], 1);
             for (int i = 0; i < 2; ++i)
-                mbar_init(&bar.s_full[i], 1), mbar_init(&bar.p_full[i], 4), mbar_init(&bar.o_full[i], 1), mbar_init(&bar.ragged[i], 1), mbar_init(&bar.clean[i], 1);
+                mbar_init(&bar.q_full[i], 1), mbar_init(&bar.s_full[i], 1), mbar_init(&bar.p_full[i], 4), mbar_init(&bar.o_full[i], 1), mbar_init(&bar.ragged[i], 1), mbar_init(&bar.clean[i], 1);
             abort_flag = 0;
             fence_barrier_init();
         }
@@ -191,11 +190,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     if (warp == 0) {
         // ---------------------------------------------------------------- producer
         if (lane == 0 && n_tiles > 0) {
-            const int q_tiles = p.two_tiles ? 2 : 1;
-            mbar_expect_tx(&bar.q_full, q_tiles * Lay::kSlabs * p.tok * p.heads * 128);
-            for (int s = 0; s < q_tiles; ++s)
-                for (int c = 0; c < Lay::kSlabs; ++c)
-                    tma_load_4d(q_smem + s * Lay::kTile + c * kSlabBytes, &maps.q, &bar.q_full, c * 64, u.q0 + t0 + s * p.tok, h0, l);
             int item = 0, slot = 0;
             uint32_t ph = 1;   // of the slot's last reader: the first round waits for nobody
             bool ok = true;
@@ -211,7 +205,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 }
             }
             // no copy of this CTA is in flight when its shared memory goes to another
-            mbar_wait(&bar.q_full, 0, &abort_flag);
             for (int i = max(0, item - kStages); i < item; ++i) mbar_wait(&bar.full[i % kStages], (i / kStages) & 1, &abort_flag);
         }
     } else if (warp == 1) {
@@ -222,7 +215,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
             constexpr uint32_t idesc_s = idesc_bf16_f32(128, 128), idesc_o = idesc_bf16_f32(128, DP) | kIdescBMn;
             constexpr uint32_t kTile16 = Lay::kTile / 16;   // descriptors count 16 bytes
             auto agree = [](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };
-            bool ok = agree(mbar_wait(&bar.q_full, 0, &abort_flag));
+            bool ok = true;
             const uint32_t q_u = smem_u32(q_smem), ring_u = smem_u32(ring);
             const uint64_t qd0 = smem_desc_sw128(q_u), qd[2] = {qd0, p.two_tiles ? qd0 + kTile16 : qd0};
             const uint64_t kd = smem_desc_sw128(ring_u), vd = smem_desc_sw128_mn(ring_u, kSlabBytes);
@@ -288,8 +281,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
             };
             const Stream<0> s0;
             const Stream<1> s1;
-            if (ok && count[0] > 0) ok = issue_s(s0);
-            if (ok && count[1] > 0) ok = issue_s(s1);
+            if (count[0] > 0) ok = agree(mbar_wait_now(&bar.q_full[0], 0, &abort_flag)) && issue_s(s0);
+            if (ok && count[1] > 0) ok = agree(mbar_wait_now(&bar.q_full[p.two_tiles], 0, &abort_flag)) && issue_s(s1);
             const int most = max(count[0], count[1]);
             for (int i = 0; ok && i < most; ++i) {
                 if (i < count[0]) ok = issue_o(s0, i);
@@ -297,6 +290,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 if (ok && i < count[1]) ok = issue_o(s1, i);
                 if (ok && i + 1 < count[1]) ok = issue_s(s1);
             }
+        }
+    } else if (warp == 3) {
+        // ---------------------------------------------------------------- queries, beside the first keys
+        if (lane == 0 && n_tiles > 0) {
+            for (int s = 0; s < (p.two_tiles ? 2 : 1); ++s) {
+                mbar_expect_tx(&bar.q_full[s], Lay::kSlabs * p.tok * p.heads * 128);
+                for (int c = 0; c < Lay::kSlabs; ++c)
+                    tma_load_4d(q_smem + s * Lay::kTile + c * kSlabBytes, &maps.q, &bar.q_full[s], c * 64, u.q0 + t0 + s * p.tok, h0, l);
+            }
+            for (int s = 0; s < (p.two_tiles ? 2 : 1); ++s) mbar_wait(&bar.q_full[s], 0, &abort_flag);
         }
     } else if (warp == 2) {
         // ---------------------------------------------------------------- V rows behind the last candidate
