@@ -1,9 +1,10 @@
 // Attention of packed query rows over [cache ; chunk] with fp32 multiply-adds: fp32 inputs, head dimensions above 128, and
 // tensors that the TMA unit cannot describe.
 //
-// A CTA takes 64 rows of one KV head (its query heads times some tokens: they share every key) and a split of its keys, 64 at a
-// time, staged as fp32.  A thread owns 4 x 4 logits, then 4 rows x D / 16 outputs; the rows' running maximum and sum are kept by the 16 threads of a
-// row group alike.  Bound by shared-memory reads (8 128-bit reads to 64 multiply-adds).
+// A CTA takes 64 rows of one KV head (its query heads times some tokens: they share every key), or 32 where few rows leave SMs without
+// work, and a split of its keys, 64 at a time, staged as fp32; fp32 tiles of up to 128 dimensions come by cp.async while the tile
+// before is worked on.  A thread owns 4 (or 2) rows of 4 logits, then of D / 16 outputs, four keys at a time; the rows' running maximum and
+// sum are kept by the 16 threads of a row group alike.  Bound by shared-memory reads (8 128-bit reads to 64 multiply-adds).
 #include "attend.cuh"
 
 namespace finch {
@@ -13,7 +14,7 @@ using tc::fma2;
 using tc::pack2;
 using tc::unpack2;
 
-constexpr int kR = kAttendSimtRows, kK = 64, kThreads = 256;
+constexpr int kK = 64;
 
 struct SimtArgs {
     ModelView mv;
@@ -32,17 +33,25 @@ __device__ __forceinline__ float4 load4f(const __nv_bfloat16 *p) {
                        __uint_as_float(v.y & 0xffff0000u));
 }
 
-template <int D>
-struct Smem {
-    static constexpr int kPitch = D + 4;
-    float q[kR * kPitch], k[kK * kPitch], v[kK * D], p[kR * (kK + 4)];
+template <bool B>
+struct Flag {
+    static constexpr bool value = B;
 };
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) attend_simt_kernel(SimtArgs p) {
+template <typename T, int D, int R>
+struct Tiles {
+    static constexpr bool kAhead = sizeof(T) == 4 && D <= 128;   // the next tile is on its way
+    static constexpr int kPitch = D + 4, kBufs = kAhead ? 2 : 1, kThreads = 256, kRows = R / 16;
+    float q[R * kPitch], k[kBufs][kK * kPitch], v[kBufs][kK * D], p[R * (kK + 4)];
+};
+
+template <typename T, int D, int R>
+__global__ void __launch_bounds__(256) attend_simt_kernel(SimtArgs p) {
     extern __shared__ __align__(16) char raw[];
-    Smem<D> &sm = *(Smem<D> *)raw;
-    constexpr int kPitch = Smem<D>::kPitch, kCols = D / 64;
+    using Mem = Tiles<T, D, R>;
+    Mem &sm = *(Mem *)raw;
+    constexpr int kPitch = Mem::kPitch, kCols = D / 64, kThreads = Mem::kThreads, kR = R, kRM = Mem::kRows;  // rows of a thread
+    constexpr bool kAhead = Mem::kAhead;
     dependency_wait();
     const ModelView &mv = p.mv;
     const int b = blockIdx.y, d = mv.d;
@@ -72,10 +81,10 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(SimtArgs p) {
                        (int64_t)(u.q0 + t0 + r % p.tok) * p.q.stride_tok + c);
         *(float4 *)(sm.q + r * kPitch + c) = v;
     }
-    int limit[4], most = 0;
+    int limit[kRM], most = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = ty * 4 + i;
+    for (int i = 0; i < kRM; ++i) {
+        const int r = ty * kRM + i;
         limit[i] = row_live(r) ? attend_limit(p.bv, u, t0 + r % p.tok, p.causal) : 0;
         most = max(most, limit[i]);
     }
@@ -88,46 +97,67 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(SimtArgs p) {
     const int tiles = (most + kK - 1) / kK;
     const int tile0 = (int)((int64_t)tiles * split / p.out.splits), tile1 = (int)((int64_t)tiles * (split + 1) / p.out.splits);
 
-    float m[4], sum[4];
-    uint64_t o[4][kCols][2];
+    float m[kRM], sum[kRM];
+    uint64_t o[kRM][kCols][2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kRM; ++i) {
         m[i] = -INFINITY, sum[i] = 0.f;
 #pragma unroll
         for (int c = 0; c < kCols; ++c) o[i][c][0] = o[i][c][1] = 0;
     }
+    // K and V rows of one tile; rows behind the last candidate and dimensions behind the head's are zeros
+    auto fetch = [&](int kt) {
+        float *ks = sm.k[kt % Mem::kBufs], *vs = sm.v[kt % Mem::kBufs];
+        for (int i = threadIdx.x; i < kK * (D / 4); i += kThreads) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4, j = kt * kK + r;
+            const bool there = c < d && j < u.N, cached = j < u.c;
+            const TensorView &k = cached ? p.ck : p.hk, &v = cached ? p.cv : p.hv;
+            const int64_t row = there ? (cached ? u.cache0 + j : u.chunk0 + j - u.c) : 0;
+            const T *from_k = (const T *)k.ptr + l * k.stride_layer + kvh * k.stride_head + row * k.stride_tok + c;
+            const T *from_v = (const T *)v.ptr + l * v.stride_layer + kvh * v.stride_head + row * v.stride_tok + c;
+            if constexpr (kAhead) {
+                if (there) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(ks + r * kPitch + c)), "l"(from_k) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(vs + r * D + c)), "l"(from_v) : "memory");
+                    continue;
+                }
+            }
+            const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+            *(float4 *)(ks + r * kPitch + c) = there ? load4f(from_k) : zero;
+            *(float4 *)(vs + r * D + c) = there ? load4f(from_v) : zero;
+        }
+        if constexpr (kAhead) asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (kAhead && tile0 < tile1) fetch(tile0);
     for (int kt = tile0; kt < tile1; ++kt) {
         const int j0 = kt * kK;
         __syncthreads();  // everyone is through with the previous tile
-        for (int i = threadIdx.x; i < kK * (D / 4); i += kThreads) {
-            const int r = i / (D / 4), c = i % (D / 4) * 4, j = j0 + r;
-            float4 k4 = make_float4(0.f, 0.f, 0.f, 0.f), v4 = k4;
-            if (c < d && j < u.N) {
-                const bool cached = j < u.c;
-                const TensorView &kt = cached ? p.ck : p.hk, &vt = cached ? p.cv : p.hv;
-                const int64_t row = cached ? u.cache0 + j : u.chunk0 + j - u.c;
-                k4 = load4f((const T *)kt.ptr + l * kt.stride_layer + kvh * kt.stride_head + row * kt.stride_tok + c);
-                v4 = load4f((const T *)vt.ptr + l * vt.stride_layer + kvh * vt.stride_head + row * vt.stride_tok + c);
-            }
-            *(float4 *)(sm.k + r * kPitch + c) = k4;
-            *(float4 *)(sm.v + r * D + c) = v4;
+        if constexpr (kAhead) {
+            if (kt + 1 < tile1) fetch(kt + 1);
+            if (kt + 1 < tile1)
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+        } else {
+            fetch(kt);
         }
         __syncthreads();
-        uint64_t acc[4][4] = {};
+        const float *ks = sm.k[kt % Mem::kBufs], *vs = sm.v[kt % Mem::kBufs];
+        uint64_t acc[kRM][4] = {};
 #pragma unroll 4
         for (int c = 0; c < d; c += 4) {
             ulonglong2 kk[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) kk[j] = *(const ulonglong2 *)(sm.k + (tx + 16 * j) * kPitch + c);
+            for (int j = 0; j < 4; ++j) kk[j] = *(const ulonglong2 *)(ks + (tx + 16 * j) * kPitch + c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const ulonglong2 qq = *(const ulonglong2 *)(sm.q + (ty * 4 + i) * kPitch + c);
+            for (int i = 0; i < kRM; ++i) {
+                const ulonglong2 qq = *(const ulonglong2 *)(sm.q + (ty * kRM + i) * kPitch + c);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[i][j] = fma2(qq.y, kk[j].y, fma2(qq.x, kk[j].x, acc[i][j]));
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kRM; ++i) {
             float s[4], top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -145,7 +175,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(SimtArgs p) {
             for (int j = 0; j < 4; ++j) {
                 s[j] = exp2f(s[j] - ref);
                 add += s[j];
-                sm.p[(ty * 4 + i) * (kK + 4) + tx + 16 * j] = s[j];
+                sm.p[(ty * kRM + i) * (kK + 4) + tx + 16 * j] = s[j];
             }
 #pragma unroll
             for (int w = 1; w < 16; w <<= 1) add += __shfl_xor_sync(0xffffffffu, add, w);
@@ -156,27 +186,41 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(SimtArgs p) {
             for (int c = 0; c < kCols; ++c) o[i][c][0] = fma2(o[i][c][0], f2, 0), o[i][c][1] = fma2(o[i][c][1], f2, 0);
         }
         __syncwarp();  // a row's weights are written and read by the same half-warp
-        const int keys = min(kK, most - j0);
-        // A key that a row does not see has weight zero there, and zero times an infinity is none: keys that are not finite
-        // everywhere are added for the rows that see them only.
-        for (int j = 0; j < keys; ++j) {
-            ulonglong2 vv[kCols];
+        // A key that a row does not see has weight zero there, and zero times an infinity is none: where some row does not see a key, keys
+        // are added for the rows that do only.
+        int seen = limit[0];
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) vv[c] = *(const ulonglong2 *)(sm.v + j * D + tx * 4 + 64 * c);
+        for (int i = 1; i < kRM; ++i) seen = min(seen, limit[i]);
+        seen -= j0;
+        const int keys = min(kK, most - j0), common = max(0, min(keys, seen)) & ~3;
+        auto add = [&](int i, float w, const ulonglong2 (&vv)[kCols]) {
+            const uint64_t w2 = pack2(w, w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = sm.p[(ty * 4 + i) * (kK + 4) + j];
-                if (j0 + j < limit[i]) {
-                    const uint64_t w2 = pack2(w, w);
+            for (int c = 0; c < kCols; ++c) o[i][c][0] = fma2(w2, vv[c].x, o[i][c][0]), o[i][c][1] = fma2(w2, vv[c].y, o[i][c][1]);
+        };
+        auto four = [&](int j, auto masked) {
+            float4 w[kRM];
 #pragma unroll
-                    for (int c = 0; c < kCols; ++c) o[i][c][0] = fma2(w2, vv[c].x, o[i][c][0]), o[i][c][1] = fma2(w2, vv[c].y, o[i][c][1]);
-                }
+            for (int i = 0; i < kRM; ++i) w[i] = *(const float4 *)(sm.p + (ty * kRM + i) * (kK + 4) + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                ulonglong2 vv[kCols];
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) vv[c] = *(const ulonglong2 *)(vs + (j + e) * D + tx * 4 + 64 * c);
+#pragma unroll
+                for (int i = 0; i < kRM; ++i)
+                    if (!decltype(masked)::value || j0 + j + e < limit[i]) add(i, e == 0 ? w[i].x : (e == 1 ? w[i].y : (e == 2 ? w[i].z : w[i].w)), vv);
             }
-        }
+        };
+        int j = 0;
+#pragma unroll 2
+        for (; j < common; j += 4) four(j, Flag<false>{});
+#pragma unroll 1
+        for (; j < keys; j += 4) four(j, Flag<true>{});
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = ty * 4 + i;
+    for (int i = 0; i < kRM; ++i) {
+        const int r = ty * kRM + i;
         if (!row_live(r)) continue;
         const int h = kvh * mv.g + h0 + r / p.tok, t = u.q0 + t0 + r % p.tok;
         const int64_t row = attend_row(mv, p.bv.total_q, l, h, t);
@@ -206,22 +250,26 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(SimtArgs p) {
     }
 }
 
-template <typename T, int D>
+template <typename T, int D, int R>
 cudaError_t launch(const Ctx &ctx, const SimtArgs &p, dim3 grid, cudaStream_t stream) {
-    const int bit = kSmemAttendSimt + (sizeof(T) == 4) + 2 * (D == 128) + 4 * (D == 256);
+    const int bit = kSmemAttendSimt + (R == 64);  // a context has one type and head dimension
     if (!ctx.smem_ready(bit)) {
-        cudaError_t e = cudaFuncSetAttribute(attend_simt_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Smem<D>));
+        cudaError_t e = cudaFuncSetAttribute(attend_simt_kernel<T, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Tiles<T, D, R>));
         if (e != cudaSuccess) return e;
         ctx.smem_set(bit);
     }
     ctx.launches += 1;
-    return launch_chained(attend_simt_kernel<T, D>, grid, dim3(kThreads), sizeof(Smem<D>), stream, p);
+    return launch_chained(attend_simt_kernel<T, D, R>, grid, dim3(256), sizeof(Tiles<T, D, R>), stream, p);
+}
+template <typename T, int R>
+cudaError_t launch_d(const Ctx &ctx, const SimtArgs &p, dim3 grid, cudaStream_t stream) {
+    if (p.mv.d <= 64) return launch<T, 64, R>(ctx, p, grid, stream);
+    if (p.mv.d <= 128) return launch<T, 128, R>(ctx, p, grid, stream);
+    return launch<T, 256, R>(ctx, p, grid, stream);
 }
 template <typename T>
-cudaError_t launch_t(const Ctx &ctx, const SimtArgs &p, dim3 grid, cudaStream_t stream) {
-    if (p.mv.d <= 64) return launch<T, 64>(ctx, p, grid, stream);
-    if (p.mv.d <= 128) return launch<T, 128>(ctx, p, grid, stream);
-    return launch<T, 256>(ctx, p, grid, stream);
+cudaError_t launch_t(const Ctx &ctx, const SimtArgs &p, int rows, dim3 grid, cudaStream_t stream) {
+    return rows == 32 ? launch_d<T, 32>(ctx, p, grid, stream) : launch_d<T, 64>(ctx, p, grid, stream);
 }
 
 }  // namespace
@@ -232,21 +280,29 @@ cudaError_t launch_attend_simt(const Ctx &ctx, const TensorView &q, const Tensor
     if (bv.batch == 0 || bv.max_q == 0) return cudaSuccess;
     const ModelView &mv = ctx.model;
     SimtArgs p = {mv, bv, q, ck, cv, hk, hv, out, ctx.d_status, causal, 0, 0, 0, 0, mv.scale * kLog2e};
-    // As many heads as share their keys, at least one token
-    p.heads = mv.g < kR ? mv.g : kR;
-    p.tok = kR / p.heads;
-    p.chunks = (mv.g + p.heads - 1) / p.heads;
-    const int tiles = (bv.max_q + p.tok - 1) / p.tok;
-    const int64_t units = (int64_t)mv.L * mv.Hkv * p.chunks;
+    // 32 rows to a CTA where there are no more, or where 64 do not give every SM one and the keys are few; more keys are split, and
+    // 64 rows read each of them less often (512 rows over 2560 keys, 8 heads: 108 us, 158 with 32 rows; 256 over 256: 19 with 32)
+    const int key_tiles = (bv.max_cache + kK - 1) / kK + (bv.max_chunk + kK - 1) / kK;
+    int64_t units = 0, tiles = 0;
+    int per_cta = (int64_t)bv.max_q * mv.g <= 32 ? 32 : kAttendSimtRows;
+    for (;; per_cta = 32) {
+        // as many heads as share their keys, at least one token
+        p.heads = mv.g < per_cta ? mv.g : per_cta;
+        p.tok = per_cta / p.heads;
+        p.chunks = (mv.g + p.heads - 1) / p.heads;
+        tiles = (bv.max_q + p.tok - 1) / p.tok;
+        units = (int64_t)mv.L * mv.Hkv * p.chunks;
+        if (per_cta == 32 || key_tiles > 8 || units * tiles * bv.batch >= ctx.sm_count) break;
+    }
+    p.row_tiles = (int)tiles;
     const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
-    int splits = attend_splits(units * tiles * bv.batch, 2 * ctx.sm_count, (bv.max_cache + bv.max_chunk + kK - 1) / kK, 2);
+    int splits = attend_splits(units * tiles * bv.batch, ctx.sm_count, key_tiles, 3);
     while (splits > 1 && splits * rows > partial_rows) --splits;
     p.out.splits = splits;
-    p.row_tiles = tiles;
     const int64_t ctas = units * splits * tiles;
     if (ctas > INT_MAX) return cudaErrorInvalidConfiguration;
     const dim3 grid((unsigned)ctas, bv.batch);
-    cudaError_t e = mv.elem_bytes == 4 ? launch_t<float>(ctx, p, grid, stream) : launch_t<__nv_bfloat16>(ctx, p, grid, stream);
+    cudaError_t e = mv.elem_bytes == 4 ? launch_t<float>(ctx, p, per_cta, grid, stream) : launch_t<__nv_bfloat16>(ctx, p, per_cta, grid, stream);
     if (e == cudaSuccess && splits > 1) e = launch_merge_splits(ctx, bv, p.out, stream);
     return e;
 }
