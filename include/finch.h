@@ -324,7 +324,7 @@ finch_status finch_rotate(finch_ctx *ctx, const finch_tensor *q, const finch_ten
  *   request's last n_q tokens); else N_b.
  * A row that sees nothing gives zeros and a log-sum-exp of -inf.  prompt_self_lse adds its term to the denominator (and to row_lse),
  * as in finch_score.  `out` has q's shape and any strides; it must not overlap an input.  row_lse may be NULL.  budget is not read;
- * row_norm must be 0.  bf16 with head_dim <= 128 runs on the tensor cores (P = exp(..) is rounded to bf16 there), everything else in
+ * row_norm must be 0 (`budget` may hold anything, but not be NULL).  bf16 with head_dim <= 128 runs on the tensor cores (P = exp(..) is rounded to bf16 there), everything else in
  * fp32 multiply-adds.  What a row does not see is not read into its result where it lies behind the request's last candidate;
  * a V row that is not finite, but is seen by some row of a request, may make rows before it not finite on the tensor cores.
  * Workspace: finch_attend_workspace_bytes, enough for every batch with no larger total_q. */
@@ -367,7 +367,8 @@ finch_status finch_pages_append(finch_ctx *ctx, const finch_pages *pages, const 
 /* out as finch_attend's, causal, over the cache's len[b] tokens: query row i of a request's n_q rows sees the first
  * len[b] - n_q + i + 1.  Made for the last token, or the last few; every 8 rows of a KV head (its query heads times tokens)
  * read the cache once.  Pages may be shared between requests.  A page number outside [0, n_pages) sets
- * FINCH_DEV_BAD_INDEX and its tokens count as not there.  row_lse may be NULL.
+ * FINCH_DEV_BAD_INDEX and its tokens count as not there.  row_lse may be NULL.  A V row that is not finite may reach rows of
+ * the same 8 that do not see it.
  * Workspace: finch_pages_workspace_bytes, the same for every call of a context (and of every context of its head_dim and device). */
 finch_status finch_pages_workspace_bytes(const finch_ctx *ctx, const finch_paged_batch *batch, size_t *out);
 finch_status finch_pages_attend(finch_ctx *ctx, const finch_pages *pages, const finch_paged_batch *batch, const finch_tensor *q,

@@ -53,8 +53,8 @@ __global__ void __launch_bounds__(kRowsPass * LPR, (sizeof(T) == 2 && !ROPE ? 76
     dependency_wait();
     const ModelView &mv = p.mv;
     const int b = blockIdx.y, groups = (mv.Hkv + p.heads_per_cta - 1) / p.heads_per_cta;
-    const int l = blockIdx.z / 2 / groups, h0 = blockIdx.z / 2 % groups * p.heads_per_cta;
-    const bool is_k = blockIdx.z % 2 == 0;
+    const int l = blockIdx.z / groups, h0 = blockIdx.z % groups * p.heads_per_cta, page0 = blockIdx.x / 2;
+    const bool is_k = blockIdx.x % 2 == 0;
     const PagedInfo u = paged_info(p.pg, p.bv, b, true);
     const bool speaks = blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0;
     const bool fits = u.ok && (u.len + u.n) / kPage <= p.pg.table_width;
@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(kRowsPass * LPR, (sizeof(T) == 2 && !ROPE ? 76
     int turn = 0;  // buffer of warp_max
     // The CTA of page 0 also takes the rows that stay open.
     const TensorView &in = is_k ? p.k : p.v;
-    for (int page = blockIdx.x; page <= full; page = blockIdx.x == 0 && page < full ? full : full + 1) {
-        if (page == full && blockIdx.x != 0) return;
+    for (int page = page0; page <= full; page = page0 == 0 && page < full ? full : full + 1) {
+        if (page == full && page0 != 0) return;
         const int first = page * kPage - waiting;          // new row in the page's first slot (negative: an open row)
         const int from = max(0, -first), to = min(kPage, u.n - first);   // slots with new rows
         if (from >= to) continue;                          // nothing stays open
@@ -209,7 +209,7 @@ cudaError_t launch(const Ctx &ctx, AppendArgs p, const finch_rope &rope, cudaStr
         }
     }
     ctx.launches += 1;
-    return launch_chained(append_kernel<T, LPR, ROPE>, dim3(pages, p.bv.batch, 2 * p.mv.L * ((p.mv.Hkv + per - 1) / per)),
+    return launch_chained(append_kernel<T, LPR, ROPE>, dim3(2 * pages, p.bv.batch, p.mv.L * ((p.mv.Hkv + per - 1) / per)),
                           dim3(kRowsPass * LPR), smem, stream, p, rope);
 }
 
