@@ -8,7 +8,7 @@
 //
 // Streams.  A CTA works on two streams at a time, a softmax warpgroup each, so that the tensor core multiplies for one while the other
 // exponentiates: two row tiles against the same keys, or, for requests of a single row tile, one row tile against the even and
-// the odd key tiles (whose results are added through shared memory at the end).
+// the odd key tiles (whose results are added through shared memory at the end).  Or two CTAs with one stream each share an SM.
 //
 // Tensor memory (512 columns): S of each stream (128), over whose first half P is written as bf16, and O of each stream.  P never leaves
 // tensor memory: it is the A operand of P V.  V tiles are B operands with their rows along K.
@@ -25,9 +25,9 @@ namespace {
 using namespace ptx;
 using namespace tc;
 
-constexpr int kTcThreads = 384;      // 4 control warps, 2 x 4 softmax warps
 constexpr float kGrowth = 8.f;       // binary orders that a row's maximum may grow before O is scaled
 constexpr int kTileRows = 128;
+constexpr int kFewTiles = 5, kManyTiles = 32;  // key tiles of one-stream CTAs: always, where every SM has work
 constexpr int kMaxCluster = 4;
 constexpr int kMaxParts = 2 * kMaxCluster;  // results of a row that meet in a cluster: its CTAs', of both streams where they share a row tile
 
@@ -51,12 +51,16 @@ struct Stream {
     static constexpr int value = S;
 };
 
-template <int DP>
+// STREAMS = 2: one CTA to an SM.  STREAMS = 1: a CTA works on one row tile, two of them share an SM (and its tensor memory), and each is
+// loaded, set up and written out under the other's work: for many short requests, where these take longer than the products.
+template <int DP, int STREAMS>
 struct Layout {
     static constexpr int kSlabs = DP / 64;
     static constexpr int kTile = kSlabs * kSlabBytes;
-    static constexpr int kStages = DP == 128 ? 5 : 8;
-    static constexpr int kBytes = (2 + kStages) * kTile + 1024;
+    static constexpr int kStages = STREAMS == 2 ? (DP == 128 ? 5 : 8) : (DP == 128 ? 2 : 5);
+    static constexpr int kBytes = (STREAMS + kStages) * kTile + 1024;
+    static constexpr int kThreads = 128 + STREAMS * 128;   // 4 control warps, 4 softmax warps to a stream
+    static constexpr int kColumns = STREAMS * 256;         // of tensor memory
 };
 
 struct Barriers {
@@ -105,19 +109,20 @@ struct Row {
     }
 };
 
-template <int DP>
-__global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TcArgs p) {
-    using Lay = Layout<DP>;
+template <int DP, int STREAMS>
+__global__ void __launch_bounds__(Layout<DP, STREAMS>::kThreads, 3 - STREAMS)
+attend_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TcArgs p) {
+    using Lay = Layout<DP, STREAMS>;
     extern __shared__ uint8_t raw[];
     __shared__ Barriers bar;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     __shared__ int limit_s[2];
     uint8_t *smem = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *q_smem = smem, *ring = smem + 2 * Lay::kTile;
+    uint8_t *q_smem = smem, *ring = smem + STREAMS * Lay::kTile;
     // a stream's result in the ring's place: O of 128 rows, then (m, l) of each
     auto box = [&](int s) { return ring + s * (DP * 512 + 1024); };
-    static_assert(2 * (DP * 512 + 1024) <= Lay::kStages * Lay::kTile, "results take the ring's place");
+    static_assert(STREAMS == 1 || 2 * (DP * 512 + 1024) <= Lay::kStages * Lay::kTile, "results take the ring's place");
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     dependency_wait();
     const ModelView &mv = p.mv;
@@ -133,7 +138,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         if (threadIdx.x == 0) atomicOr(p.status, FINCH_DEV_BAD_BATCH);
         return;
     }
-    const int t0 = tile * (p.two_tiles ? 2 : 1) * p.tok;
+    const bool two_tiles = STREAMS == 2 && p.two_tiles;
+    const int t0 = tile * (two_tiles ? 2 : 1) * p.tok;
     if (t0 >= u.n_q) return;
     const int h0 = kvh * mv.g + hc * p.heads, n_heads = min(p.heads, mv.g - hc * p.heads);
 
@@ -148,13 +154,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
             fence_barrier_init();
         }
     } else if (warp == 1) {
-        tmem_alloc(&tmem_slot, 512);
+        tmem_alloc(&tmem_slot, Lay::kColumns);
         tmem_relinquish();
     } else {
         const int s = warp - 2;
-        if (s < 2) {
+        if (s < STREAMS) {
             int most = 0;
-            const int ts = t0 + (p.two_tiles ? s * p.tok : 0);
+            const int ts = t0 + (two_tiles ? s * p.tok : 0);
             for (int i = lane; i < p.tok; i += 32)
                 if (ts + i < u.n_q) most = max(most, attend_limit(p.bv, u, ts + i, p.causal));
             most = __reduce_max_sync(0xffffffffu, most);
@@ -171,22 +177,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     auto tiles_for = [&](int limit) {
         return limit <= u.c ? (limit + kTileRows - 1) / kTileRows : cache_tiles + (limit - u.c + kTileRows - 1) / kTileRows;
     };
-    const int all0 = tiles_for(limit_s[0]), all1 = tiles_for(limit_s[1]), all = max(all0, all1);
+    const int all0 = tiles_for(limit_s[0]), all1 = STREAMS == 2 ? tiles_for(limit_s[1]) : 0, all = max(all0, all1);
     const int begin = (int)((int64_t)all * split / p.out.splits), end = (int)((int64_t)all * (split + 1) / p.out.splits);
     const int n_tiles = end - begin;                    // loaded
     int count[2];                                        // of each stream
-    if (p.two_tiles) {
+    if (STREAMS == 1) {
+        count[0] = n_tiles, count[1] = 0;
+    } else if (two_tiles) {
         count[0] = max(0, min(end, all0) - begin), count[1] = max(0, min(end, all1) - begin);
     } else {
         count[0] = (n_tiles + 1) / 2, count[1] = n_tiles / 2;
     }
-    const bool gathers = p.cluster > 1 || (!p.two_tiles && count[1] > 0);   // rows' results meet others in shared memory
-    auto tile_of = [&](int s, int i) { return p.two_tiles ? i : 2 * i + s; };  // in the split
+    const bool gathers = STREAMS == 2 && (p.cluster > 1 || (!two_tiles && count[1] > 0));   // rows' results meet others in shared memory
+    auto tile_of = [&](int s, int i) { return two_tiles || STREAMS == 1 ? i : 2 * i + s; };  // in the split
     // the last stream to use a tile frees it
-    auto frees = [&](int s, int t) { return !p.two_tiles || s == 1 || t >= count[1]; };
+    auto frees = [&](int s, int t) { return !two_tiles || s == 1 || t >= count[1]; };
     constexpr int kStages = Lay::kStages;
 
-    if (warp < 4) regs_dec<104>();
+    if (warp < 4) regs_dec<STREAMS == 2 ? 104 : 72>();
     if (warp == 0) {
         // ---------------------------------------------------------------- producer
         if (lane == 0 && n_tiles > 0) {
@@ -217,12 +225,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
             auto agree = [](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };
             bool ok = true;
             const uint32_t q_u = smem_u32(q_smem), ring_u = smem_u32(ring);
-            const uint64_t qd0 = smem_desc_sw128(q_u), qd[2] = {qd0, p.two_tiles ? qd0 + kTile16 : qd0};
+            const uint64_t qd0 = smem_desc_sw128(q_u), qd[2] = {qd0, two_tiles ? qd0 + kTile16 : qd0};
             const uint64_t kd = smem_desc_sw128(ring_u), vd = smem_desc_sw128_mn(ring_u, kSlabBytes);
             // the tiles whose V rows are cleared behind the last token: the cache's last, the chunk's last
             const int ragged0 = u.c % kTileRows ? cache_tiles - 1 - begin : -1;
             const int ragged1 = u.m % kTileRows ? cache_tiles + (u.m + kTileRows - 1) / kTileRows - 1 - begin : -1;
-            const int step = p.two_tiles ? 2 : 4;           // items from a stream's tile to its next
+            const int step = two_tiles || STREAMS == 1 ? 2 : 4;           // items from a stream's tile to its next
             // slot and phase of each stream's next K and V item
             int k_slot[2], v_slot[2], tile_k[2], tile_v[2];
             uint32_t k_ph[2] = {0, 0}, v_ph[2] = {0, 0}, p_ph[2] = {0, 0};
@@ -252,7 +260,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 __syncwarp();
                 tile_k[s] += step / 2;
                 k_slot[s] += step;
-                if (k_slot[s] >= kStages) k_slot[s] -= kStages, k_ph[s] ^= 1;
+                while (k_slot[s] >= kStages) k_slot[s] -= kStages, k_ph[s] ^= 1;
                 return true;
             };
             auto issue_o = [&](auto stream, int i) {
@@ -268,7 +276,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kTileRows / 16; ++k)
-                        umma_bf16_tmem(tmem + 256 + s * DP, tmem + s * 128 + k * 8, b_desc + k * (2048 / 16), idesc_o, i > 0 || k > 0);
+                        umma_bf16_tmem(tmem + STREAMS * 128 + s * DP, tmem + s * 128 + k * 8, b_desc + k * (2048 / 16), idesc_o, i > 0 || k > 0);
                     if (last) umma_commit(&bar.empty[v_slot[s]]);
                     if (end) umma_commit(&bar.o_full[s]);
                 }
@@ -276,30 +284,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 p_ph[s] ^= 1;
                 tile_v[s] += step / 2;
                 v_slot[s] += step;
-                if (v_slot[s] >= kStages) v_slot[s] -= kStages, v_ph[s] ^= 1;
+                while (v_slot[s] >= kStages) v_slot[s] -= kStages, v_ph[s] ^= 1;
                 return true;
             };
             const Stream<0> s0;
             const Stream<1> s1;
             if (count[0] > 0) ok = agree(mbar_wait_now(&bar.q_full[0], 0, &abort_flag)) && issue_s(s0);
-            if (ok && count[1] > 0) ok = agree(mbar_wait_now(&bar.q_full[p.two_tiles], 0, &abort_flag)) && issue_s(s1);
+            if (STREAMS == 2 && ok && count[1] > 0) ok = agree(mbar_wait_now(&bar.q_full[two_tiles], 0, &abort_flag)) && issue_s(s1);
             const int most = max(count[0], count[1]);
             for (int i = 0; ok && i < most; ++i) {
                 if (i < count[0]) ok = issue_o(s0, i);
                 if (ok && i + 1 < count[0]) ok = issue_s(s0);
-                if (ok && i < count[1]) ok = issue_o(s1, i);
-                if (ok && i + 1 < count[1]) ok = issue_s(s1);
+                if (STREAMS == 2 && ok && i < count[1]) ok = issue_o(s1, i);
+                if (STREAMS == 2 && ok && i + 1 < count[1]) ok = issue_s(s1);
             }
         }
     } else if (warp == 3) {
         // ---------------------------------------------------------------- queries, beside the first keys
         if (lane == 0 && n_tiles > 0) {
-            for (int s = 0; s < (p.two_tiles ? 2 : 1); ++s) {
+            for (int s = 0; s < (two_tiles ? 2 : 1); ++s) {
                 mbar_expect_tx(&bar.q_full[s], Lay::kSlabs * p.tok * p.heads * 128);
                 for (int c = 0; c < Lay::kSlabs; ++c)
                     tma_load_4d(q_smem + s * Lay::kTile + c * kSlabBytes, &maps.q, &bar.q_full[s], c * 64, u.q0 + t0 + s * p.tok, h0, l);
             }
-            for (int s = 0; s < (p.two_tiles ? 2 : 1); ++s) mbar_wait(&bar.q_full[s], 0, &abort_flag);
+            for (int s = 0; s < (two_tiles ? 2 : 1); ++s) mbar_wait(&bar.q_full[s], 0, &abort_flag);
         }
     } else if (warp == 2) {
         // ---------------------------------------------------------------- V rows behind the last candidate
@@ -321,11 +329,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         }
     } else if (warp >= 4) {
         // ---------------------------------------------------------------- softmax
-        regs_inc<200>();
-        const int s = (warp - 4) / 4, quarter = warp % 4, r = quarter * 32 + lane;
+        regs_inc<STREAMS == 2 ? 200 : 184>();
+        const int s = STREAMS == 2 ? (warp - 4) / 4 : 0, quarter = warp % 4, r = quarter * 32 + lane;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-        const uint32_t st = tmem + s * 128 + lane_base, ot = tmem + 256 + s * DP + lane_base;
-        const int hr = r / p.tok, tr = t0 + (p.two_tiles ? s * p.tok : 0) + r % p.tok;
+        const uint32_t st = tmem + s * 128 + lane_base, ot = tmem + STREAMS * 128 + s * DP + lane_base;
+        const int hr = r / p.tok, tr = t0 + (two_tiles ? s * p.tok : 0) + r % p.tok;
         const bool live = hr < n_heads && tr < u.n_q;
         const int limit = live ? attend_limit(p.bv, u, tr, p.causal) : u.N;
         // columns of tile t (of the request) that this row sees: one of these minus 128 t
@@ -404,7 +412,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         tc_fence_after();
         const float m2 = m * p.scale2;   // the reference in base-2 logits (-inf: none of the row's keys)
         if (!gathers) {
-            Row row(p, u, l, h0 + hr, tr, live && (p.two_tiles || s == 0), split);
+            Row row(p, u, l, h0 + hr, tr, live && (two_tiles || s == 0), split);
             row.finish(m2, sum);
 #pragma unroll 1
             for (int c = 0; c < mv.d; c += 16) {
@@ -420,7 +428,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                 row.put(c + 8, y + 8);
                 __syncwarp();
             }
-        } else {
+        } else if constexpr (STREAMS == 2) {
             // the pages' place is free when the other stream's MMAs are complete, too
             if (count[1 - s] > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait_now(&bar.o_full[1 - s], 0, &abort_flag));
             tc_fence_after();
@@ -439,7 +447,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         }
         tc_fence_before();
     }
-    if (gathers) {
+    if constexpr (STREAMS == 2) if (gathers) {
         // ---- the streams and the CTAs that worked on the same rows: every CTA adds all of them for some columns
         __syncwarp();
         if (p.cluster > 1) {
@@ -450,7 +458,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
         }
         if (warp >= 4) {
             const int rank = split % p.cluster, r = warp % 4 * 32 + lane;
-            const int sets = p.two_tiles ? 2 : 1, parts = p.two_tiles ? p.cluster : 2 * p.cluster;
+            const int sets = two_tiles ? 2 : 1, parts = two_tiles ? p.cluster : 2 * p.cluster;
             const uint32_t box0 = smem_u32(box(0)), box1 = smem_u32(box(1));
             auto add = [&](auto remote) {
                 constexpr bool kRemote = decltype(remote)::value == 1;
@@ -458,8 +466,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
                     const int hr = r / p.tok, tr = t0 + set * p.tok + r % p.tok;
                     Row row(p, u, l, h0 + hr, tr, hr < n_heads && tr < u.n_q, split / p.cluster);
                     auto part_at = [&](int j) {
-                        const uint32_t at = (p.two_tiles ? set : j % 2) ? box1 : box0;
-                        return kRemote ? map_to_rank(at, p.two_tiles ? j : j / 2) : at;
+                        const uint32_t at = (two_tiles ? set : j % 2) ? box1 : box0;
+                        return kRemote ? map_to_rank(at, two_tiles ? j : j / 2) : at;
                     };
                     float m[kMaxParts], f[kMaxParts], ref = -INFINITY, total = 0.f;
 #pragma unroll
@@ -519,21 +527,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_tc_kernel(const __grid_c
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(tmem, Lay::kColumns);
     }
     if (threadIdx.x == 0 && abort_flag) atomicOr(p.status, FINCH_DEV_TIMEOUT);
 }
 
-template <int DP>
+template <int DP, int STREAMS>
 cudaError_t launch(const Ctx &ctx, const Maps &maps, const TcArgs &p, dim3 grid, cudaStream_t stream) {
-    const int bit = kSmemAttendTc + (DP == 128);
+    using Lay = Layout<DP, STREAMS>;
+    const int bit = kSmemAttendTc + (STREAMS == 2);   // a context has one head dimension
     if (!ctx.smem_ready(bit)) {
-        cudaError_t e = cudaFuncSetAttribute(attend_tc_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<DP>::kBytes);
+        cudaError_t e = cudaFuncSetAttribute(attend_tc_kernel<DP, STREAMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kBytes);
         if (e != cudaSuccess) return e;
         ctx.smem_set(bit);
     }
     ctx.launches += 1;
-    return launch_chained_cluster(attend_tc_kernel<DP>, p.cluster, grid, dim3(kTcThreads), Layout<DP>::kBytes, stream, maps, p);
+    return launch_chained_cluster(attend_tc_kernel<DP, STREAMS>, p.cluster, grid, dim3(Lay::kThreads), Lay::kBytes, stream, maps, p);
 }
 
 // A map of a row tile's queries: one box is `tok` tokens of `heads` heads.
@@ -592,7 +601,12 @@ cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorVi
     // Two row tiles to a CTA, unless that leaves more than half of the SMs without one.
     const int64_t units = (int64_t)mv.L * mv.Hkv * p.chunks, one_tile = units * bv.batch * ((bv.max_q + p.tok - 1) / p.tok);
     p.two_tiles = bv.max_q > p.tok && 2 * one_tile > ctx.sm_count;
-    const int per_cta = p.two_tiles ? 2 * p.tok : p.tok;
+    const int key_tiles = (bv.max_cache + kTileRows - 1) / kTileRows + (bv.max_chunk + kTileRows - 1) / kTileRows;
+    // One row tile to a CTA, two CTAs to an SM, where the keys are few, or not many and every SM has work (rows of 32 KV heads: 16 requests
+    // of up to 512 66 us with two streams to a CTA, 51 with one; 64 of up to 64 97 and 48; 512 rows 15.9 and 14.3; but 64 rows of 4 requests
+    // over 4160 keys 38 and 51, 1024 rows over 5120 87 and 90, 8192 rows of 8 KV heads 463 and 471)
+    const bool one_stream = key_tiles <= kFewTiles || (key_tiles <= kManyTiles && one_tile > ctx.sm_count);
+    const int per_cta = p.two_tiles && !one_stream ? 2 * p.tok : p.tok;
     p.row_tiles = (bv.max_q + per_cta - 1) / per_cta;
     Maps maps;
     if (!make_q_map(&maps.q, q, mv.d, bv.total_q, mv.Hq, mv.L, p.tok, p.heads)) return cudaErrorNotSupported;
@@ -607,12 +621,15 @@ cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorVi
     if (!cache) maps.ck = maps.cv = maps.q;
     if (!chunk) maps.hk = maps.hv = maps.q;
     const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
-    const int key_tiles = (bv.max_cache + kTileRows - 1) / kTileRows + (bv.max_chunk + kTileRows - 1) / kTileRows;
-    choose_splits(ctx.sm_count, units * p.row_tiles * bv.batch, key_tiles, p.two_tiles, partial_rows / (rows > 0 ? rows : 1), p.cluster, p.out.splits);
+    if (!one_stream) choose_splits(ctx.sm_count, units * p.row_tiles * bv.batch, key_tiles, p.two_tiles, partial_rows / (rows > 0 ? rows : 1), p.cluster, p.out.splits);
     const int64_t ctas = units * p.out.splits * p.row_tiles;
     if (ctas > INT_MAX) return cudaErrorInvalidConfiguration;
     const dim3 grid((unsigned)ctas, bv.batch);
-    cudaError_t e = mv.d <= 64 ? launch<64>(ctx, maps, p, grid, stream) : launch<128>(ctx, maps, p, grid, stream);
+    cudaError_t e;
+    if (one_stream)
+        e = mv.d <= 64 ? launch<64, 1>(ctx, maps, p, grid, stream) : launch<128, 1>(ctx, maps, p, grid, stream);
+    else
+        e = mv.d <= 64 ? launch<64, 2>(ctx, maps, p, grid, stream) : launch<128, 2>(ctx, maps, p, grid, stream);
     p.out.splits /= p.cluster;
     if (e == cudaSuccess && p.out.splits > 1) e = launch_merge_splits(ctx, bv, p.out, stream);
     return e;
