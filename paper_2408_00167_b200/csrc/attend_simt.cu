@@ -1,9 +1,9 @@
 // Attention of packed query rows over [cache ; chunk] with fp32 multiply-adds: fp32 inputs, head dimensions above 128, and
 // tensors that the TMA unit cannot describe.
 //
-// A CTA takes 64 rows of one KV head (its query heads times some tokens: they share every key), or 32 where few rows leave SMs without
-// work, and a split of its keys, 64 at a time, staged as fp32; fp32 tiles of up to 128 dimensions come by cp.async while the tile
-// before is worked on.  A thread owns 4 (or 2) rows of 4 logits, then of D / 16 outputs, four keys at a time; the rows' running maximum and
+// A CTA takes 64 rows of one KV head (its query heads times some tokens: they share every key), or 32 or 16 where few rows leave SMs
+// without work, and a split of its keys, 64 at a time, staged as fp32; fp32 tiles of up to 128 dimensions come by cp.async while the tile
+// before is worked on.  A thread owns 4 (2, 1) rows of 4 logits, then of D / 16 outputs, four keys at a time; the rows' running maximum and
 // sum are kept by the 16 threads of a row group alike.  Bound by shared-memory reads (8 128-bit reads to 64 multiply-adds).
 #include "attend.cuh"
 
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(256) attend_simt_kernel(SimtArgs p) {
 
 template <typename T, int D, int R>
 cudaError_t launch(const Ctx &ctx, const SimtArgs &p, dim3 grid, cudaStream_t stream) {
-    const int bit = kSmemAttendSimt + (R == 64);  // a context has one type and head dimension
+    const int bit = kSmemAttendSimt + (R == 64) + 2 * (R == 32);  // a context has one type and head dimension
     if (!ctx.smem_ready(bit)) {
         cudaError_t e = cudaFuncSetAttribute(attend_simt_kernel<T, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Tiles<T, D, R>));
         if (e != cudaSuccess) return e;
@@ -269,6 +269,7 @@ cudaError_t launch_d(const Ctx &ctx, const SimtArgs &p, dim3 grid, cudaStream_t 
 }
 template <typename T>
 cudaError_t launch_t(const Ctx &ctx, const SimtArgs &p, int rows, dim3 grid, cudaStream_t stream) {
+    if (rows == 16) return launch_d<T, 16>(ctx, p, grid, stream);
     return rows == 32 ? launch_d<T, 32>(ctx, p, grid, stream) : launch_d<T, 64>(ctx, p, grid, stream);
 }
 
@@ -280,23 +281,24 @@ cudaError_t launch_attend_simt(const Ctx &ctx, const TensorView &q, const Tensor
     if (bv.batch == 0 || bv.max_q == 0) return cudaSuccess;
     const ModelView &mv = ctx.model;
     SimtArgs p = {mv, bv, q, ck, cv, hk, hv, out, ctx.d_status, causal, 0, 0, 0, 0, mv.scale * kLog2e};
-    // 32 rows to a CTA where there are no more, or where 64 do not give every SM one and the keys are few; more keys are split, and
-    // 64 rows read each of them less often (512 rows over 2560 keys, 8 heads: 108 us, 158 with 32 rows; 256 over 256: 19 with 32)
+    // 64 rows to a CTA, fewer where there are no more, or where that leaves most SMs without one and the keys are few (8 heads of 64: 16 rows
+    // over 16 8.9 us with 64, 5.4 with 16; 256 over 256 19.0, 14.7 with 32, 16.8 with 16; 512 over 512 29, 35, 38; 100 over 2148 35, 43, 65)
     const int key_tiles = (bv.max_cache + kK - 1) / kK + (bv.max_chunk + kK - 1) / kK;
     int64_t units = 0, tiles = 0;
-    int per_cta = (int64_t)bv.max_q * mv.g <= 32 ? 32 : kAttendSimtRows;
-    for (;; per_cta = 32) {
+    int per_cta = kAttendSimtRows;
+    for (;; per_cta /= 2) {
         // as many heads as share their keys, at least one token
         p.heads = mv.g < per_cta ? mv.g : per_cta;
         p.tok = per_cta / p.heads;
         p.chunks = (mv.g + p.heads - 1) / p.heads;
         tiles = (bv.max_q + p.tok - 1) / p.tok;
         units = (int64_t)mv.L * mv.Hkv * p.chunks;
-        if (per_cta == 32 || key_tiles > 8 || units * tiles * bv.batch >= ctx.sm_count) break;
+        const bool fits = (int64_t)bv.max_q * mv.g * 2 <= per_cta, idle = key_tiles <= 4 && units * tiles * bv.batch < ctx.sm_count / 4;
+        if (per_cta == 16 || !(fits || idle)) break;
     }
     p.row_tiles = (int)tiles;
     const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
-    int splits = attend_splits(units * tiles * bv.batch, ctx.sm_count, key_tiles, 3);
+    int splits = attend_splits(units * tiles * bv.batch, ctx.sm_count, key_tiles, 2);
     while (splits > 1 && splits * rows > partial_rows) --splits;
     p.out.splits = splits;
     const int64_t ctas = units * splits * tiles;
