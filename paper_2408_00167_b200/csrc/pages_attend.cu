@@ -86,12 +86,14 @@ struct Shares {
 struct Place {
     int b, groups;  // groups: of Shares
     int64_t in_front, total;
+    Request r;
 };
 __device__ __forceinline__ Place find_items(const DecodeArgs &p) {
     const int lane = threadIdx.x & 31, batch = p.bv.batch;
-    Place place = {0, 1, 0, 0};
+    Place place;
+    place.b = 0, place.groups = 1, place.in_front = place.total = 0;
     if (batch == 1) {
-        const Request r = request_of(p, 0);
+        const Request r = place.r = request_of(p, 0);
         if (!r.u.ok && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, FINCH_DEV_BAD_BATCH);
         place.total = r.all_items();
         if (r.units > 0 && gridDim.x % r.units == 0) place.groups = r.units;
@@ -135,12 +137,14 @@ __device__ __forceinline__ Place find_items(const DecodeArgs &p) {
                 if (who) {
                     place.b = __shfl_sync(0xffffffffu, hit, __ffs(who) - 1);
                     place.in_front = __shfl_sync(0xffffffffu, hit_at, __ffs(who) - 1);
+                    place.r = request_of(p, place.b);
                     return place;
                 }
             }
         }
         place.total = before;
     }
+    place.r.units = 0;
     return place;  // no items at all
 }
 
@@ -381,7 +385,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
     if (at >= end) return;
     int b = place.b;
     int64_t in_front = place.in_front;
-    Request req = request_of(p, b);
+    Request req = place.r;
 
     for (int piece = 0; at < end; ++piece) {
         while (at >= in_front + req.all_items()) {  // the next request that has work
@@ -706,16 +710,16 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
         if (whole) continue;
         // ---- the CTA that delivers a unit's last piece adds them
         const int c0 = shares.of(unit_at), c1 = shares.of(unit_at + items - 1);
-        __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
-            const int n = atomicAdd(p.pieces + c0, 1);
+            // releases the CTA's pieces, which the barrier has put in front of it, and acquires those of the CTAs before
+            int n;
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(p.pieces + c0) : "memory");
             last_s = n == c1 - c0;
             if (last_s) p.pieces[c0] = 0;  // nobody else comes
         }
         __syncthreads();
         if (!last_s) continue;
-        __threadfence();
         for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
             const int r = i / (D / 4), c = i % (D / 4) * 4;
             auto slot_of = [&](int cta) { return (2 * (int64_t)cta + (shares.begin(cta) < unit_at)) * kRows + r; };
