@@ -1,17 +1,19 @@
 // Attention of a request's newest tokens over its paged 8-bit cache (pages.cuh).
 //
-// Bound by the bytes of the cache: a page and KV head are 2 x 64 x d bytes that 8 query rows share.  A warp takes whole pages straight
-// from global memory into the registers of mma.sync fragments, 16 bytes a lane and load: which dimension is which k index is free as
-// long as both operands agree, and so is the order of the keys and, for the output, of the rows.  Codes turn into f16 exactly (two
+// Bound by the bytes of the cache: a page and KV head are 2 x 64 x d bytes that 8 query rows share.  A warp copies whole pages
+// into three slots of shared memory of its own (two on their way while one is read) and reads them as mma.sync fragments, 16 bytes a
+// lane: which dimension is which k index is free as long as both operands agree, and so is the order of the keys and, for the output,
+// of the rows.  Codes turn into f16 exactly (two
 // at a time); of V, whose pairs along k are two keys, bytes of two rows are interleaved first.
 //
-//   S^T = K Q^T   16 keys x 8 query rows.  Rows of Q are f16 after a power of two took their range: exact for bf16 inputs; fp32 inputs
-//                 enter as two f16 parts, 22 bits.  Page and row scales multiply the logits.
-//   O^T += V^T P^T  16 dimensions x 8 rows.  P = 2^(s - m) in [0, 1] enters as two f16 parts, turned from the layout of S^T by
-//                 movmatrix; a page's product is folded into O (fp32) with its V scale.
+//   S^T = K Q^T   16 keys x 8 query rows.  Rows of Q are f16 after a power of two took their range: exact for bf16 elements down to
+//                 2^-30 of the row's largest; fp32 inputs enter as two f16 parts, 22 bits down to 2^-16 of it, 2^-38 of it at the least.
+//                 Page and row scales multiply the logits.
+//   O^T += V^T P^T  16 dimensions x 8 rows.  P = 2^(s - m) in [0, 1] enters, lifted, as two f16 parts, turned from the layout of S^T
+//                 by movmatrix; a page's product is folded into O (fp32) with its V scale.
 //
-// (tcgen05 wants 128 rows and its operands in shared memory: 8 rows would waste 15/16 of it and every code would make a second trip
-// through shared memory.)  The open rows go the same way, 16 to a warp: bf16 as they are, fp32 as f16 parts scaled by a power of two.
+// (tcgen05 wants 128 rows and its operands in shared memory: 8 rows would waste 15/16 of it and every code would go through shared
+// memory once more, as f16.)  The open rows go the same way, 16 to a warp, in bf16: bf16 as they are, fp32 as three parts.
 //
 // The work is a list of items: for every request, layer, KV head and group of 8 rows (a unit) its full pages, then one for the open
 // rows.  A CTA takes an equal share of consecutive items: all CTAs have the same number of pages, whatever the lengths.  A unit within
@@ -24,6 +26,10 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32, kRows = kPagesRows;
 constexpr int kCtasPerSm = 2;
+// P in [0, 1] is lifted by 2^15 where it becomes f16: weights down to 2^-18 of the largest keep 22 bits, smaller ones are off by at
+// most 2^-40 of it, so that a long cache's many small weights add up.  Q's elements, scaled into [1, 2) by the row's largest, are
+// lifted by 2^13 likewise.
+constexpr float kLift = 32768.f, kDrop = 1.f / kLift, kLiftLog2 = 15.f, kQueryLift = 8192.f;
 constexpr int kScan = 4;   // requests of a lane and step of the search for a CTA's items
 
 struct DecodeArgs {
@@ -179,10 +185,10 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t 
     const float2 h = __half22float2(*(const __half2 *)&hi);
     lo = half2_of(x - h.x, y - h.y);
 }
-// The power of two at or below a magnitude's, and its inverse, where both are normal numbers.
+// The power of two at or below a magnitude's, and its inverse, where both are normal numbers, also after the lift.
 __device__ __forceinline__ void power_of_two(float top, float &up, float &down) {
     int ex = (int)(__float_as_uint(top) >> 23) - 127;
-    ex = top > 0.f ? max(-126, min(126, ex)) : 0;
+    ex = top > 0.f ? max(-110, min(126, ex)) : 0;
     up = __uint_as_float((uint32_t)(127 + ex) << 23);
     down = __uint_as_float((uint32_t)(127 - ex) << 23);
 }
@@ -264,7 +270,7 @@ struct Running {
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = 0.f;
     }
     // Softmax step over NT tiles of 16 keys: s[t] = logits of (key gid, rows 2 tid, 2 tid + 1), (key gid + 8, ..) become P; corr: the
-    // factors of what was before.
+    // factors of what was before.  P and sum are lifted, o is not.
     template <int NT>
     __device__ __forceinline__ void weights(float (&s)[NT][4], float (&corr)[2]) {
         float now[2] = {m[0], m[1]}, ref[2];
@@ -278,6 +284,7 @@ struct Running {
             for (int x = 4; x < 32; x <<= 1) now[r] = fmaxf(now[r], __shfl_xor_sync(0xffffffffu, now[r], x));
             ref[r] = now[r] == -INFINITY ? 0.f : now[r];
             corr[r] = tc::ex2(m[r] - ref[r]);
+            ref[r] -= kLiftLog2;
             m[r] = now[r];
             sum[r] *= corr[r];  // a lane's own keys only: the lanes' sums are added at the end
         }
@@ -314,54 +321,80 @@ __device__ __forceinline__ void mma16816_bf16(float (&c)[4], uint32_t a0, uint32
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 16 open rows of bf16, as they are: K and Q multiply exactly, P enters as three bf16 parts, 24 bits.  Keys key0 + gid (+ 8) of the
-// slot, `rest` of which hold tokens; j0 the token of key0 + gid.
-template <int D>
-__device__ __forceinline__ void open_rows_bf16(Running<D> &run, const __nv_bfloat16 *q, bool live, const __nv_bfloat16 *k, const __nv_bfloat16 *v,
-                                               int key0, int rest, int j0, const int (&lim)[2], float scale2) {
+// x, y -> N parts of bf16, 8 bits each with the range of fp32; an infinity is its first part.
+template <int N>
+__device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&w)[N]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        w[n] = *(const uint32_t *)&h;
+        const float hx = __uint_as_float(w[n] << 16), hy = __uint_as_float(w[n] & 0xffff0000u);
+        x = fabsf(hx) == INFINITY ? 0.f : x - hx, y = fabsf(hy) == INFINITY ? 0.f : y - hy;
+    }
+}
+// Four neighbouring elements as pairs of parts: one part of bf16, three of fp32 (24 bits, no common power of two: rows that differ
+// by any order, or that a query row does not see, leave one another alone).
+__device__ __forceinline__ void load_parts(const __nv_bfloat16 *p, bool there, uint32_t (&w)[2][1]) {
+    const uint2 x = there ? __ldg((const uint2 *)p) : make_uint2(0, 0);
+    w[0][0] = x.x, w[1][0] = x.y;
+}
+__device__ __forceinline__ void load_parts(const float *p, bool there, uint32_t (&w)[2][3]) {
+    const float4 x = there ? __ldg((const float4 *)p) : make_float4(0.f, 0.f, 0.f, 0.f);
+    split_bf16(x.x, x.y, w[0]);
+    split_bf16(x.z, x.w, w[1]);
+}
+
+// 16 open rows: bf16 enters as it is, fp32 and P as three bf16 parts (products of parts below 2^-24 are left out).  Keys key0 + gid
+// (+ 8) of the slot, `rest` of which hold tokens; j0 the token of key0 + gid.
+template <typename T, int D>
+__device__ __forceinline__ void open_rows(Running<D> &run, const T *q, bool live, const T *k, const T *v, int key0, int rest, int j0,
+                                          const int (&lim)[2], float scale2) {
+    constexpr int N = sizeof(T) == 4 ? 3 : 1;
     const int lane = threadIdx.x & 31, gid = lane >> 2, tid = lane & 3;
-    const uint2 none = make_uint2(0, 0);
     const int ka = key0 + gid, kb = ka + 8;
     float s[1][4] = {{0.f, 0.f, 0.f, 0.f}}, corr[2];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {  // four dimensions of the lane: 16 i + 4 tid
         const int e = 16 * i + 4 * tid;
-        const uint2 x = ka < rest ? __ldg((const uint2 *)(k + ka * D + e)) : none, y = kb < rest ? __ldg((const uint2 *)(k + kb * D + e)) : none;
-        const uint2 z = live ? __ldg((const uint2 *)(q + e)) : none;
-        mma16816_bf16(s[0], x.x, y.x, x.y, y.y, z.x, z.y);
+        uint32_t x[2][N], y[2][N], z[2][N];
+        load_parts(k + ka * D + e, ka < rest, x);
+        load_parts(k + kb * D + e, kb < rest, y);
+        load_parts(q + e, live, z);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int m = 0; m + n < N; ++m) mma16816_bf16(s[0], x[0][n], y[0][n], x[1][n], y[1][n], z[0][m], z[1][m]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[0][i] = j0 + i / 2 * 8 < lim[i % 2] ? s[0][i] * scale2 : -INFINITY;
     run.weights(s, corr);
-    uint32_t pf[3][2];
+    uint32_t pf[2][3];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        float x = s[0][2 * h], y = s[0][2 * h + 1];
+        split_bf16(s[0][2 * h], s[0][2 * h + 1], pf[h]);
 #pragma unroll
-        for (int n = 0; n < 3; ++n) {
-            const __nv_bfloat162 w = __floats2bfloat162_rn(x, y);
-            const uint32_t bits = *(const uint32_t *)&w;
-            x -= __uint_as_float(bits << 16), y -= __uint_as_float(bits & 0xffff0000u);
-            pf[n][h] = transposed(bits);
+        for (int n = 0; n < 3; ++n) pf[h][n] = transposed(pf[h][n]);
+    }
+#pragma unroll
+    for (int e = 0; e < D / 8; e += 4) {
+        uint32_t w[4][2][N];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int key = key0 + tid * 2 + i / 2 * 8 + i % 2;
+            load_parts(v + key * D + gid * (D / 8) + e, key < rest, w[i]);
         }
-    }
-    constexpr int kW = D / 16;  // words of a lane's D / 8 dimensions
-    uint32_t w[4][kW];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int key = key0 + tid * 2 + i / 2 * 8 + i % 2;
+        for (int j = 0; j < 2; ++j) {
+            float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < kW; ++e) w[i][e] = 0;
-        if (key < rest) load_words<kW>(w[i], v + key * D + gid * (D / 8));
-    }
+            for (int n = 0; n < N; ++n) {
+                const uint32_t a0 = __byte_perm(w[0][j][n], w[1][j][n], 0x5410), a1 = __byte_perm(w[0][j][n], w[1][j][n], 0x7632);
+                const uint32_t a2 = __byte_perm(w[2][j][n], w[3][j][n], 0x5410), a3 = __byte_perm(w[2][j][n], w[3][j][n], 0x7632);
 #pragma unroll
-    for (int e = 0; e < kW; ++e) {
-        const uint32_t a0 = __byte_perm(w[0][e], w[1][e], 0x5410), a1 = __byte_perm(w[0][e], w[1][e], 0x7632);
-        const uint32_t a2 = __byte_perm(w[2][e], w[3][e], 0x5410), a3 = __byte_perm(w[2][e], w[3][e], 0x7632);
-        float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int n = 0; n < 3; ++n) mma16816_bf16(c, a0, a1, a2, a3, pf[n][0], pf[n][1]);
-        run.fold(2 * e, c, 1.f, corr);
+                for (int m = 0; m + n < 3; ++m) mma16816_bf16(c, a0, a1, a2, a3, pf[0][m], pf[1][m]);
+            }
+            run.fold(e + 2 * j, c, kDrop, corr);
+        }
     }
 }
 
@@ -457,7 +490,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             float big, down;
             power_of_two(top, big, down);
-            big *= p.scale2;
+            down *= kQueryLift, big *= p.scale2 / kQueryLift;
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
                 two_of<T>(w, i, x, y);
@@ -477,7 +510,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
             for (int n = 0; n < n_mine; ++n) {
                 const float f[2] = {up[0] * k_scale, up[1] * k_scale};
                 const bool skip = !good(n0);
-                const float vs = skip ? 0.f : v_scale;
+                const float vs = skip ? 0.f : v_scale * kDrop;
                 if (skip && lane == 0) atomicOr(p.status, FINCH_DEV_BAD_INDEX);
                 if (n + 1 < n_mine) k_scale = __ldg(p.pg.k_scale + place_of(n1)), v_scale = __ldg(p.pg.v_scale + place_of(n1));
                 copies_wait<2>();
@@ -576,91 +609,9 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
         if (key0 < rest) {
             const int64_t open = p.pg.open_row(mv, l, u.slot, kvh) * D;
             const int j0 = u.len - rest + key0 + gid;
-            if constexpr (!kTwoParts) {
-                open_rows_bf16<D>(run, (const __nv_bfloat16 *)p.q.ptr + l * p.q.stride_layer + (int64_t)(kvh * mv.g + (rg * kRows + gid) % mv.g) * p.q.stride_head +
-                                           (int64_t)(u.row0 + token(gid)) * p.q.stride_tok,
-                                  gid < rows, (const __nv_bfloat16 *)p.pg.open_k + open, (const __nv_bfloat16 *)p.pg.open_v + open, key0, rest, j0, lim,
-                                  p.scale2);
-            } else {
-            float s[1][4], big, down, top = 0.f, x, y;
-            {
-                uint32_t w[2][D / 4 / kWordsT];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int key = key0 + gid + 8 * h;
-                    const T *src = (const T *)p.pg.open_k + open + key * D + tid * Geo::kVec;
-#pragma unroll
-                    for (int i = 0; i < D / 4 / kWordsT; ++i) w[h][i] = 0;
-                    if (key < rest) {
-#pragma unroll
-                        for (int c = 0; c < Geo::kChunks; ++c) load_words<Geo::kVec / kWordsT>(&w[h][c * Geo::kVec / kWordsT], src + c * 4 * Geo::kVec);
-                    }
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        two_of<T>(w[h], i, x, y);
-                        top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
-                    }
-                }
-#pragma unroll
-                for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-                power_of_two(top, big, down);
-                float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < Geo::kSteps; ++i) {
-                    uint32_t a[4], r[4];
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        two_of<T>(w[h % 2], 2 * i + h / 2, x, y);
-                        split2(x * down, y * down, a[h], r[h]);
-                    }
-                    mma16816(c, a[0], a[1], a[2], a[3], qh[i][0], qh[i][1]);
-                    if constexpr (kTwoParts) {
-                        mma16816(c, a[0], a[1], a[2], a[3], ql[i][0], ql[i][1]);
-                        mma16816(c, r[0], r[1], r[2], r[3], qh[i][0], qh[i][1]);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[0][i] = j0 + i / 2 * 8 < lim[i % 2] ? c[i] * (up[i % 2] * big) : -INFINITY;
-            }
-            uint32_t hi[1][2], lo[1][2];
-            float corr[2];
-            run.weights(s, corr);
-            run.parts(s, hi, lo);
-            uint32_t w[4][D / 8 / kWordsT];
-            top = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = key0 + tid * 2 + i / 2 * 8 + i % 2;
-#pragma unroll
-                for (int e = 0; e < D / 8 / kWordsT; ++e) w[i][e] = 0;
-                if (key < rest) load_words<D / 8 / kWordsT>(w[i], (const T *)p.pg.open_v + open + key * D + gid * (D / 8));
-#pragma unroll
-                for (int e = 0; e < D / 16; ++e) {
-                    two_of<T>(w[i], e, x, y);
-                    top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
-                }
-            }
-#pragma unroll
-            for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-            power_of_two(top, big, down);
-#pragma unroll
-            for (int e = 0; e < D / 16; ++e) {  // dimensions 2e and 2e + 1
-                float v[4][2];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    two_of<T>(w[i], e, v[i][0], v[i][1]);
-                    v[i][0] *= down, v[i][1] *= down;
-                }
-                uint32_t a[4], r[4];
-#pragma unroll
-                for (int h = 0; h < 4; ++h) split2(v[h / 2 * 2][h % 2], v[h / 2 * 2 + 1][h % 2], a[h], r[h]);
-                float c[4] = {0.f, 0.f, 0.f, 0.f};
-                mma16816(c, a[0], a[1], a[2], a[3], hi[0][0], hi[0][1]);
-                mma16816(c, a[0], a[1], a[2], a[3], lo[0][0], lo[0][1]);
-                if constexpr (kTwoParts) mma16816(c, r[0], r[1], r[2], r[3], hi[0][0], hi[0][1]);
-                run.fold(2 * e, c, big, corr);
-            }
-            }
+            open_rows<T, D>(run, (const T *)p.q.ptr + l * p.q.stride_layer + (int64_t)(kvh * mv.g + (rg * kRows + gid) % mv.g) * p.q.stride_head +
+                                     (int64_t)(u.row0 + token(gid)) * p.q.stride_tok,
+                            gid < rows, (const T *)p.pg.open_k + open, (const T *)p.pg.open_v + open, key0, rest, j0, lim, p.scale2);
         }
 
         // ---- the warps of the CTA in their order; a thread has four dimensions of a row
@@ -668,7 +619,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
         for (int r = 0; r < 2; ++r) {
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) run.sum[r] += __shfl_xor_sync(0xffffffffu, run.sum[r], x);
-            if (gid == 0) part_ml[warp][2 * tid + r] = make_float2(run.m[r], run.sum[r]);
+            if (gid == 0) part_ml[warp][2 * tid + r] = make_float2(run.m[r], run.sum[r] * kDrop);
 #pragma unroll
             for (int i = 0; i < D / 8; i += 4)
                 *(float4 *)(part(warp, 2 * tid + r) + gid * (D / 8) + i) = make_float4(run.o[i][r], run.o[i + 1][r], run.o[i + 2][r], run.o[i + 3][r]);

@@ -381,3 +381,92 @@ def test_the_same_result_in_a_graph_with_lengths_that_grow_on_the_device():
         assert lens[0].tolist() == c.lens and fb.finch_device_status(c.ctx) == 0
     finally:
         c.close()
+
+
+def _filled(k, v, dtype, Hq=1):
+    """A cache of one request and layer that holds rows k and v, [Hkv][len][d]."""
+    import torch
+    Hkv, n, d = k.shape
+    c = Cache(1, Hq, Hkv, d, 1, (n + PAGE - 1) // PAGE, dtype)
+    rows = [x[None].to(c.dtype).contiguous() for x in (k, v)]
+    fb.finch_pages_append(c.ctx, c.pages, fb.make_paged_batch([0], new_off=[0, n]), *rows)
+    c.lens = [n]
+    return c
+
+
+def _attend_rows(c, q, see=None):
+    """Rows q [Hq][n][d] over the cache of `_filled`: every weight counts by its own size, every logit by its own sum of magnitudes.
+    see: the rows that are checked (all)."""
+    import torch
+    from attend_reference import attend_rows, check_rows
+    n = q.shape[1]
+    q = q[None].to(c.dtype).contiguous()
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:3], math.nan, device="cuda")
+    batch = fb.make_paged_batch(c.lens, q_off=[0, n])
+    ws = torch.empty(fb.finch_pages_workspace_bytes(c.ctx, batch), dtype=torch.uint8, device="cuda")
+    fb.finch_pages_attend(c.ctx, c.pages, batch, q, out, lse, ws=ws)
+    assert fb.finch_device_status(c.ctx) == 0
+    k, v = c.values(0)
+    see = range(n) if see is None else see
+    for h in range(c.Hq):
+        kv = h // (c.Hq // c.Hkv)
+        for i in see:
+            # a weight enters with 22 bits: 2^-21 of itself at most (2^-20 leaves room for its exponential), where that is above half a
+            # step of the smallest f16 numbers, 2^-25, under a lift of 2^15: 2^-40 of the largest weight, itself at most 1
+            want = list(attend_rows(q[0, h, i:i + 1], k[0, kv], v[0, kv], [c.lens[0] - n + i + 1], 1 / math.sqrt(c.d), None, 2.0 ** -20))
+            want[2] = want[2] + 2.0 ** -40 * v[0, kv, :c.lens[0] - n + i + 1].abs().sum(0)
+            check_rows(out[0, h, i:i + 1], lse[0, h, i:i + 1], *want, what=f"head {h} row {i}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [40, 64, 150, 4000])
+def test_many_small_weights_add_up(dtype, n):
+    """One key in 64 takes nearly all the weight and has values of zero: what is left are weights of 2^-26 and below."""
+    import torch
+    k, v = torch.zeros((1, n, 64), device="cuda"), torch.ones((1, n, 64), device="cuda")
+    k[:, 5::64, 0], v[:, 5::64] = 16.0, 0.0
+    q = torch.zeros((1, 1, 64), device="cuda")
+    for size in (9.0, 10.0, 11.0):       # weights of 2^-26, 2^-29 and 2^-32
+        c = _filled(k, v, dtype)
+        try:
+            q[..., 0] = size
+            _attend_rows(c, q)
+        finally:
+            c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [40, 100])
+def test_a_row_does_not_feel_the_size_of_keys_behind_it(dtype, n):
+    """Open rows that the first query rows do not see: very large, or with keys that are not numbers."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn((1, n, 64), generator=g, device="cuda") for _ in range(2))
+    q = torch.randn((1, 5, 64), generator=g, device="cuda")
+    k[:, -2], v[:, -2:] = 1e25, -1e25
+    for last in (1e30, math.inf, math.nan):
+        k[:, -1] = last
+        c = _filled(k, v, dtype)
+        try:
+            _attend_rows(c, q, see=range(3))
+        finally:
+            c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [40, 64, 150])
+def test_rows_with_a_few_large_elements(dtype, n):
+    """A query element thousands of times the others where keys are zero, and an open key and value likewise."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(4)
+    k, v = (torch.randn((2, n, 96), generator=g, device="cuda") for _ in range(2))
+    q = torch.randn((4, 2, 96), generator=g, device="cuda")
+    k[..., 7], q[..., 7] = 0.0, 20000.0
+    if n % PAGE:
+        k[:, -1, 11], q[..., 11] = 30000.0, 0.0
+        v[:, -3, 13] = 20000.0
+    c = _filled(k, v, dtype, Hq=4)
+    try:
+        _attend_rows(c, q)
+    finally:
+        c.close()
