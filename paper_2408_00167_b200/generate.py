@@ -37,7 +37,7 @@ class PagedCache:
         import torch
         self.torch, self.device, self.rope = torch, device, rope
         self.L, self.Hq, self.Hkv, self.d, self.B = n_layers, n_q_heads, n_kv_heads, head_dim, batch
-        self.max_tokens = max_tokens
+        self.max_tokens, self.max_step = max_tokens, max(max_step, 1)
         width = -(-max_tokens // fb.FINCH_PAGE_TOKENS)
         tdtype = torch.float32 if dtype == fb.FINCH_F32 else torch.bfloat16
         page = (fb.FINCH_PAGE_TOKENS, head_dim)
@@ -51,7 +51,7 @@ class PagedCache:
         # a layer's calls see that layer's part of every array
         self._of_layer = [fb.make_pages(*(t[l:l + 1] for t in self._tensors), self.table, self.slot) for l in range(n_layers)]
         index = torch.device(device).index or 0
-        bounds = dict(max_batch=max(batch, 1), max_prompt=max(max_step, 1), max_candidates=max(max_tokens, 1), device=index)
+        bounds = dict(max_batch=max(batch, 1), max_prompt=self.max_step, max_candidates=max(max_tokens, 1), device=index)
         self._ctx_all = fb.finch_ctx_create(n_layers, n_q_heads, n_kv_heads, head_dim, dtype, scale=scale, **bounds)
         self._ctx = fb.finch_ctx_create(1, n_q_heads, n_kv_heads, head_dim, dtype, scale=scale, **bounds)
         self.len = np.zeros(batch, dtype=np.int32)
@@ -85,6 +85,8 @@ class PagedCache:
 
     def step(self, tokens: int = 1) -> None:
         """`tokens` more of every request: appends and attention of all layers follow, then the next step."""
+        if not 1 <= tokens <= self.max_step:
+            raise ValueError(f"PagedCache.step: {tokens} tokens, 1 to {self.max_step} (max_step) can be one step")
         if int(self.len.max(initial=0)) + tokens > self.max_tokens:
             raise ValueError(f"PagedCache.step: room for {self.max_tokens} tokens")
         off = np.arange(self.B + 1, dtype=np.int32) * tokens
@@ -96,8 +98,12 @@ class PagedCache:
 
     def append(self, layer: int, k, v) -> None:
         """The step's new rows of a layer, [1][n_kv_heads][batch * tokens][head_dim], requests one behind the other."""
+        if self._add is None:
+            raise ValueError("PagedCache.append: no step has been begun")
         fb.finch_pages_append(self._ctx, self._of_layer[layer], self._add, k, v, rope=self.rope)
 
     def attend(self, layer: int, q, out, row_lse=None) -> None:
         """Attention of the step's query rows, [1][n_q_heads][batch * tokens][head_dim], over the layer's cache."""
+        if self._see is None:
+            raise ValueError("PagedCache.attend: no step has been begun")
         fb.finch_pages_attend(self._ctx, self._of_layer[layer], self._see, q, out, row_lse, ws=self._ws)

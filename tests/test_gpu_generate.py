@@ -122,3 +122,19 @@ def test_steps_of_several_tokens_and_a_batch_without_a_document():
             check_rows(out[0, h, 2 * b:2 * b + 2], None, *want)
     assert cache.status() == 0
     cache.close()
+
+
+def test_calls_out_of_order():
+    import torch
+    x = torch.zeros((1, 2, 1, 64), device="cuda")
+    cache = PagedCache(1, 2, 2, 64, fb.FINCH_F32, 1, max_tokens=4, max_step=2)
+    try:
+        for call in (lambda: cache.append(0, x, x), lambda: cache.attend(0, x, x.clone()), lambda: cache.step(3), lambda: cache.step(0)):
+            with pytest.raises(ValueError):
+                call()
+        cache.step()
+        cache.append(0, x, x)
+        cache.attend(0, x, x.clone())
+        assert cache.status() == 0 and cache.len.tolist() == [1]
+    finally:
+        cache.close()
