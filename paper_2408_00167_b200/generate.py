@@ -96,14 +96,21 @@ class PagedCache:
         if self._ws is None:
             self._ws = self.torch.empty(fb.finch_pages_workspace_bytes(self._ctx, self._see), dtype=self.torch.uint8, device=self.device)
 
+    def _check_rows(self, what: str, t, heads: int) -> None:
+        if t.shape != (1, heads, self._add.c.total_new, self.d):
+            raise ValueError(f"PagedCache.{what}: expected rows {(1, heads, self._add.c.total_new, self.d)}, got {tuple(t.shape)}")
+
     def append(self, layer: int, k, v) -> None:
         """The step's new rows of a layer, [1][n_kv_heads][batch * tokens][head_dim], requests one behind the other."""
         if self._add is None:
             raise ValueError("PagedCache.append: no step has been begun")
+        self._check_rows("append", k, self.Hkv)
+        self._check_rows("append", v, self.Hkv)
         fb.finch_pages_append(self._ctx, self._of_layer[layer], self._add, k, v, rope=self.rope)
 
     def attend(self, layer: int, q, out, row_lse=None) -> None:
         """Attention of the step's query rows, [1][n_q_heads][batch * tokens][head_dim], over the layer's cache."""
         if self._see is None:
             raise ValueError("PagedCache.attend: no step has been begun")
+        self._check_rows("attend", q, self.Hq)
         fb.finch_pages_attend(self._ctx, self._of_layer[layer], self._see, q, out, row_lse, ws=self._ws)

@@ -135,6 +135,10 @@ def test_calls_out_of_order():
         cache.step()
         cache.append(0, x, x)
         cache.attend(0, x, x.clone())
+        two = torch.zeros((1, 2, 2, 64), device="cuda")
+        for call in (lambda: cache.append(0, two, two), lambda: cache.append(0, x, x[:, :1]), lambda: cache.attend(0, two, two.clone())):
+            with pytest.raises(ValueError):
+                call()
         assert cache.status() == 0 and cache.len.tolist() == [1]
     finally:
         cache.close()
