@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kRotThreads, 4) rotate_kernel(RotateArgs p, co
         const int64_t src_step = step * in.stride_head, dst_step = step * out.stride_head;
         Eight<T> x[kAhead];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) x[a].zero();  // a lane behind the row's end adds nothing to its sum
+        for (int a = 0; a < kAhead; ++a) x[a].zero();
         for (; first < h_last; first += kAhead * step) {
 #pragma unroll
             for (int a = 0; a < kAhead; ++a) {
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kRotThreads, 4) rotate_kernel(RotateArgs p, co
                     }
                     float sum, odd;
                     tc::unpack2(sum2, sum, odd);
-                    sum += odd;
+                    sum = live ? sum + odd : 0.f;  // a lane behind the row's end adds nothing, whatever a row that was not finite left in it
 #pragma unroll
                     for (int m = 1; m < LPR; m <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
                     const float r = rsqrtf(fmaf(sum, inv_d, p.eps));

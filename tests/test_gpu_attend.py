@@ -339,3 +339,36 @@ def test_rotate_in_place_in_a_packed_projection():
     fb.finch_rotate(ctx, q, k, pos, q, k, rope=rope)
     assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(buf[:, :, Hq + Hkv:], before[:, :, Hq + Hkv:])
     fb.finch_ctx_destroy(ctx)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rotary,pairing", [(96, 0, 0), (96, 96, 0), (160, 64, 1), (192, 192, 0), (224, 224, 1)])
+def test_a_head_that_is_not_finite_stays_alone(dtype, d, rotary, pairing):
+    """A head of zeros with eps = 0, and one with a NaN, in head dimensions that leave lanes of a row unused; enough tokens that a warp
+    walks a token's heads in several rounds.  Every other head is what it is without them, bit for bit."""
+    import torch
+    tdtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+    L, Hq, Hkv, tokens = 2, 24, 12, 1250
+    g = torch.Generator(device="cuda").manual_seed(d)
+    q, k = (torch.randn((L, h, tokens, d), generator=g, device="cuda").to(tdtype) for h in (Hq, Hkv))
+    w = [(1 + 0.2 * torch.randn((L, d), generator=g, device="cuda")).to(tdtype) for _ in range(2)]
+    pos = torch.randint(0, 100000, (tokens,), generator=g, device="cuda").to(torch.int32)
+    rope = fb.finch_rope_init(rotary, fb.finch_rope_frequencies(rotary), pairing) if rotary else None
+    ctx = fb.finch_ctx_create(L, Hq, Hkv, d, fb.FINCH_BF16 if dtype == "bf16" else fb.FINCH_F32)
+
+    def run(q, k):
+        out = [torch.full_like(x, math.nan) for x in (q, k)]
+        fb.finch_rotate(ctx, q, k, pos, *out, rope=rope, q_weight=w[0], k_weight=w[1], eps=0.0)
+        return out
+
+    clean = run(q, k)
+    for bad in (0.0, math.nan, math.inf):
+        dirty = [q.clone(), k.clone()]
+        for x in dirty:
+            x[:, 1] = 0.0 if bad == 0.0 else x[:, 1]
+            x[:, 1, ::3, 5] = bad
+        for got, want in zip(run(*dirty), clean):
+            others = [h for h in range(want.shape[1]) if h != 1]
+            assert torch.isfinite(want.float()).all()
+            assert torch.equal(got[:, others], want[:, others])
+    fb.finch_ctx_destroy(ctx)
