@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
         const uint32_t mine_u = ptx::smem_u32(mine);
         auto number_of = [&](int n) { return n < n_mine ? __ldg(table + item0 + warp + n * kWarps) : 0; };
         auto good = [&](int number) { return number >= 0 && number < p.pg.n_pages; };
-        auto place_of = [&](int number) { return p.pg.page_head(mv, l, good(number) ? number : 0, kvh); };  // what is read of a bad one does not count
+        auto place_of = [&](int number) { return p.pg.page_head(mv, l, good(number) ? number : 0, kvh); };  // of a bad one nothing enters the result
         auto fetch = [&](int n, int number, bool is_v) {   // K or V of this warp's n-th page
             if (n < n_mine) {
                 const uint8_t *src = (is_v ? p.pg.v : p.pg.k) + place_of(number) * Geo::kSlot;
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
             for (int n = 0; n < n_mine; ++n) {
                 const float f[2] = {up[0] * k_scale, up[1] * k_scale};
                 const bool skip = !good(n0);
-                const float vs = skip ? 0.f : v_scale * kDrop;
+                const float vs = v_scale * kDrop;
                 if (skip && lane == 0) atomicOr(p.status, FINCH_DEV_BAD_INDEX);
                 if (n + 1 < n_mine) k_scale = __ldg(p.pg.k_scale + place_of(n1)), v_scale = __ldg(p.pg.v_scale + place_of(n1));
                 copies_wait<2>();
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(DecodeArgs p) {
                 run.parts(s, hi, lo);
                 copies_wait<2>();
                 __syncwarp();
-                {
+                if (!skip) {  // weights of zero take no NaN out: a refused page leaves the result (of which corr is 1, or which is 0) as it is
                     const uint32_t slot = mine_u + (2 * n + 1) % Geo::kSlots * Geo::kSlot;
                     constexpr int kW = Geo::kWords, kHalf = kW > 4 ? kW / 2 : kW;   // words at a time (accumulators: 8 registers a word)
                     static_assert(kW % kHalf == 0 || kW == 5 || kW == 7, "");

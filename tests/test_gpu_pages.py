@@ -470,3 +470,36 @@ def test_rows_with_a_few_large_elements(dtype, n):
         _attend_rows(c, q)
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,length,bad_pages,rows", [(64, 200, [1], 1), (96, 200, [0, 2], 3), (128, 64, [0], 1), (256, 700, [3, 9], 2), (128, 5000, [0, 7, 70], 4)])
+def test_a_refused_page_is_not_there_whatever_page_0_holds(dtype, d, length, bad_pages, rows):
+    """Page 0 is nobody's and holds NaN codes and scales; a unit with refused pages has the result of the pages that are left."""
+    import torch
+    from attend_reference import attend_rows, check_rows
+    c = Cache(1, 4, 1, d, 1, (length + PAGE - 1) // PAGE, dtype)
+    try:
+        spare = next(n for n in range(1, c.k.shape[1]) if n not in set(c.table.flatten().tolist()))
+        c.table[c.table == 0] = spare
+        c.append([length])
+        k, v = c.values(0)
+        for i, w in enumerate(bad_pages):
+            c.table[0, w] = (-1, c.k.shape[1], 2 ** 31 - 1)[i % 3]
+        q = torch.randn((1, 4, rows, d), generator=c.g, device="cuda").to(c.dtype)
+        out, lse = torch.full_like(q, math.nan), torch.full((1, 4, rows), math.nan, device="cuda")
+        batch = fb.make_paged_batch([length], q_off=[0, rows])
+        ws = torch.empty(fb.finch_pages_workspace_bytes(c.ctx, batch), dtype=torch.uint8, device="cuda")
+        fb.finch_pages_attend(c.ctx, c.pages, batch, q, out, lse, ws=ws)
+        assert fb.finch_device_status(c.ctx) == fb.FINCH_DEV_BAD_INDEX
+        for h in range(4):
+            for i in range(rows):
+                there = [j for j in range(length - rows + i + 1) if j // PAGE not in bad_pages]
+                # as in Cache.attend: queries and weights enter the products with 22 bits
+                want = list(attend_rows(q[0, h, i:i + 1], k[0, 0, there], v[0, 0, there], [len(there)], 1 / math.sqrt(d), None, 2.0 ** -20))
+                if there:
+                    big = q[0, h, i:i + 1].double().abs().amax(-1) * k[0, 0].abs().sum(-1).max() / math.sqrt(d) * 2.0 ** -21
+                    want[3], want[2] = want[3] + big, want[2] + 2 * big[:, None] * v[0, 0].abs().amax()
+                check_rows(out[0, h, i:i + 1], lse[0, h, i:i + 1], *want, what=f"head {h} row {i}")
+    finally:
+        c.close()
