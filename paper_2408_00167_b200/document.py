@@ -89,18 +89,20 @@ class DocumentCompressor:
 
     def verify(self) -> None:
         """Wait for the steps enqueued so far and check them: raises RuntimeError when the device status word is set
-        or when the lengths on the device differ from the host mirror the later steps were sized with."""
+        or when the lengths on the device differ from the host mirror the later steps were sized with.  The mirror then takes the
+        device's lengths: rows that a refused step would have written are not counted again."""
         if self._unverified == 0:
             return
         self._unverified = 0
         word = fb.finch_device_status(self.ctx)            # synchronises the stream
         dev_len = self._bufs[self._cur]["len"][:self.B].cpu().numpy()
+        expected, self.cache_len = self.cache_len, dev_len.astype(np.int32)
         if word != 0:
             raise RuntimeError(f"document loop: device status word {word:#x} after {self.steps} steps "
-                               f"(lengths on the device {dev_len.tolist()}, expected {self.cache_len.tolist()})")
-        if not np.array_equal(dev_len, self.cache_len):
+                               f"(lengths on the device {dev_len.tolist()}, expected {expected.tolist()})")
+        if not np.array_equal(dev_len, expected):
             raise RuntimeError(f"document loop: cache lengths on the device {dev_len.tolist()} differ from the "
-                               f"host mirror {self.cache_len.tolist()} after {self.steps} steps")
+                               f"host mirror {expected.tolist()} after {self.steps} steps")
 
     def reset(self) -> None:
         """Start a new batch of documents in the same buffers (empty caches).  Checks the finished one first."""

@@ -70,7 +70,11 @@ class PagedCache:
 
     def fill(self, doc: DocumentCompressor) -> None:
         """The compressed caches of `doc` become the requests' first tokens, all layers, one call for each request (a request's
-        kept rows need not fill its part of the compressor's buffers).  Nothing is rotated: kept keys stand at their slots."""
+        kept rows need not fill its part of the compressor's buffers).  Nothing is rotated: kept keys stand at their slots.
+
+        Waits for the compressor's steps: its lengths on the host are a prediction, and rows of a step that the device refused do
+        not exist.  Raises RuntimeError then, as DocumentCompressor.verify does."""
+        doc.verify()
         if (doc.L, doc.Hkv, doc.d, doc.B) != (self.L, self.Hkv, self.d, self.B):
             raise ValueError("PagedCache.fill: another model or batch")
         if int(doc.cache_len.max(initial=0)) > self.max_tokens:

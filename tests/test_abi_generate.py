@@ -275,3 +275,22 @@ def test_the_binding_refuses_other_types_shapes_and_devices(lib, ctx):
         fb.make_paged_batch([10], new_off=[0, 5], len_tensor=torch.zeros(1), device="cpu")
 
 
+def test_a_cache_checks_the_document_that_fills_it(monkeypatch):
+    """fill asks the compressor before it believes the lengths on the host, and moves nothing if that raises."""
+    from paper_2408_00167_b200.generate import PagedCache
+    moved = []
+    monkeypatch.setattr(fb, "finch_pages_append", lambda *a, **k: moved.append(a))
+
+    class Refused:
+        L = Hkv = d = B = 1
+        cache_len = np.array([3], dtype=np.int32)
+
+        def verify(self):
+            raise RuntimeError("status word")
+
+    cache = PagedCache.__new__(PagedCache)
+    cache.L = cache.Hkv = cache.d = cache.B = 1
+    cache.max_tokens, cache.len = 64, np.zeros(1, dtype=np.int32)
+    with pytest.raises(RuntimeError):
+        cache.fill(Refused())
+    assert not moved and cache.len.tolist() == [0]

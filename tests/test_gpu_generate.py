@@ -142,3 +142,24 @@ def test_calls_out_of_order():
         assert cache.status() == 0 and cache.len.tolist() == [1]
     finally:
         cache.close()
+
+
+def test_a_document_whose_step_was_refused_does_not_become_a_cache():
+    """The compressor's lengths on the host are a prediction; a step that the device refused has written no rows."""
+    import torch
+    L, Hq, Hkv, d = 1, 4, 2, 64
+    doc = DocumentCompressor(L, Hq, Hkv, d, fb.FINCH_BF16, [32], max_prompt=8, max_chunk=100)
+    cache = PagedCache(L, Hq, Hkv, d, fb.FINCH_BF16, 1, max_tokens=64)
+    try:
+        rows = lambda h, n: torch.randn((L, h, n, d), device="cuda").to(torch.bfloat16)
+        doc._bufs[doc._cur]["len"].fill_(1)                  # the host's bound on the cache is 0
+        doc.step(rows(Hq, 8), [0, 8], rows(Hkv, 100), rows(Hkv, 100), torch.arange(100, dtype=torch.int32, device="cuda"), [0, 100], [32])
+        assert doc.cache_len.tolist() == [32]
+        with pytest.raises(RuntimeError):
+            cache.fill(doc)
+        assert cache.len.tolist() == [0] and cache.status() == 0
+        cache.fill(doc)                                      # again: there is nothing to move
+        assert doc.cache_len.tolist() == [0] and cache.len.tolist() == [0]
+    finally:
+        cache.close()
+        doc.close()
