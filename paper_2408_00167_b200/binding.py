@@ -234,6 +234,9 @@ def finch_ctx_create(n_layers, n_q_heads, n_kv_heads, head_dim, dtype, group_mod
                        max_candidates, device, rope_theta, rope_pairing)
     ctx = C.c_void_p()
     _check(load().finch_ctx_create(C.byref(cfg), C.byref(ctx)), "finch_ctx_create")
+    # what the operators' tensors have to be: a call takes addresses and strides, the sizes are the context's
+    ctx.model = n_layers, n_q_heads, n_kv_heads, head_dim, int(dtype), int(device)
+    ctx.pages = n_layers, n_kv_heads, head_dim, int(dtype), int(device)
     return ctx
 
 
@@ -339,6 +342,22 @@ def finch_step_host(ctx, host_prompt_q, host_chunk_k, host_chunk_v, host_chunk_p
 
 # ------------------------------------------------------------------ rotation, attention, the paged 8-bit cache
 
+def _model(what: str, ctx, like, q, kv):
+    """(n_layers, n_q_heads, n_kv_heads, head_dim) of a context, which `like` has to fit in type and device.  Of a handle that
+    finch_ctx_create of this module has not made, the tensors' own sizes have to do."""
+    m = getattr(ctx, "model", None)
+    if m is None:
+        shapes = [t.shape for t in (q, kv) if t is not None]
+        if not shapes or any(len(s) != 4 for s in shapes):
+            raise ValueError(f"{what}: expected [layers][heads][tokens][head_dim] tensors")
+        return shapes[0][0], shapes[0][1], shapes[-1][1], shapes[0][3]
+    L, Hq, Hkv, d, code, device = m
+    dtype = (_dtypes or _dtypes_of())[2 + code]
+    if like.dtype != dtype or (device >= 0 and like.get_device() != device):
+        raise ValueError(f"{what}: the context is for {dtype} on device {device}, got {like.dtype} on {like.device}")
+    return L, Hq, Hkv, d
+
+
 def _views_like(what: str, like, *tensors):
     """_views of tensors that have to be on `like`'s device and of its dtype: a kernel would read the bits of another one all the
     same.  The checks of a call are most of what it takes on the host, hence one pass over the tensors."""
@@ -363,6 +382,21 @@ def _views_like(what: str, like, *tensors):
     return buf, C.addressof(buf)
 
 
+def _holds(what: str, shape, want) -> None:
+    """A tensor of four axes has `want`'s sizes, and rows at least: a kernel reads and writes behind the end of one that has fewer."""
+    if want[2] and (len(shape) != 4 or shape[2] < want[2] or (shape[0], shape[1], shape[3]) != (want[0], want[1], want[3])):
+        raise ValueError(f"{what}: expected {want} or more rows, got {tuple(shape)}")
+
+
+def _space(what: str, ws, like):
+    """Address and bytes of a workspace on `like`'s device."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != like.get_device() or not ws.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous workspace on {like.device}, got one on {ws.device}")
+    return ws.data_ptr() or None, ws.numel() * ws.element_size()
+
+
 def _array(what: str, t, dtype, like, shape):
     """Address of a contiguous tensor of the given dtype and shape on `like`'s device; None: none."""
     if t is None:
@@ -373,6 +407,12 @@ def _array(what: str, t, dtype, like, shape):
     return t.data_ptr() or None
 
 
+def _rows_of(what: str, t, dtype, like, n: int, dense: bool) -> None:
+    """An array of the batch description: n entries, or (not dense: one for each row) at least so many."""
+    if t.dtype != dtype or t.get_device() != like.get_device() or not t.is_contiguous() or t.numel() < n or (dense and t.numel() != n):
+        raise ValueError(f"{what}: expected {n} contiguous {dtype} on {like.device}, got {t.dtype} of {tuple(t.shape)} on {t.device}")
+
+
 def _same_shape(what: str, t, shape) -> None:
     if t.shape != shape:
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
@@ -381,11 +421,12 @@ def _same_shape(what: str, t, shape) -> None:
 _dtypes = None
 
 
-def _i32_f32():
+def _dtypes_of():
+    """int32, float32, and the types of FINCH_F32 and FINCH_BF16."""
     global _dtypes
     if _dtypes is None:
         import torch
-        _dtypes = torch.int32, torch.float32
+        _dtypes = torch.int32, torch.float32, torch.float32, torch.bfloat16
     return _dtypes
 
 
@@ -419,16 +460,18 @@ def finch_rotate(ctx, q, k, pos, out_q, out_k, rope: Optional[finch_rope] = None
     if like is None or (q is None) != (out_q is None) or (k is None) != (out_k is None):
         raise ValueError("finch_rotate: q, k or both, each with its output")
     keep, v = _views_like("finch_rotate", like, q, k, out_q, out_k)
+    L, Hq, Hkv, d = _model("finch_rotate", ctx, like, q, k)
     shape = like.shape
-    L, _, tokens, d = shape
+    tokens = shape[2]
     if q is not None:
-        _same_shape("finch_rotate: out_q", out_q, shape)
+        if shape != (L, Hq, tokens, d) or out_q.shape != shape:
+            raise ValueError(f"finch_rotate: expected q and out_q of {(L, Hq, tokens, d)}, got {tuple(shape)}, {tuple(out_q.shape)}")
     if k is not None:
-        if k is not like and (k.shape[0] != L or k.shape[2] != tokens or k.shape[3] != d):
-            raise ValueError(f"finch_rotate: k is {tuple(k.shape)}, q {tuple(shape)}")
-        _same_shape("finch_rotate: out_k", out_k, k.shape)
+        shape = k.shape
+        if shape != (L, Hkv, tokens, d) or out_k.shape != shape:
+            raise ValueError(f"finch_rotate: expected k and out_k of {(L, Hkv, tokens, d)}, got {tuple(shape)}, {tuple(out_k.shape)}")
     z, dtype = _VIEW_BYTES, like.dtype
-    _check(load().finch_rotate(ctx, v, v + z, tokens, _array("finch_rotate: pos", pos, _i32_f32()[0], like, (tokens,)), _rope(rope),
+    _check(load().finch_rotate(ctx, v, v + z, tokens, _array("finch_rotate: pos", pos, _dtypes_of()[0], like, (tokens,)), _rope(rope),
                                _array("finch_rotate: q_weight", q_weight, dtype, like, (L, d)),
                                _array("finch_rotate: k_weight", k_weight, dtype, like, (L, d)), eps, v + 2 * z, v + 3 * z,
                                _stream(stream)), "finch_rotate")
@@ -442,13 +485,34 @@ def finch_attend_workspace_bytes(ctx, batch: Batch) -> int:
 
 def finch_attend(ctx, q, cache_k, cache_v, chunk_k, chunk_v, batch: Batch, out, row_lse=None, causal: bool = True, ws=None,
                  stream=None) -> None:
-    """Attention of the packed query rows over [cache ; chunk] (see the header); `out` has q's shape."""
+    """Attention of the packed query rows over [cache ; chunk] (see the header).  Tensors hold the batch's rows (total_q, total_cache,
+    total_chunk) or more; `out` has q's shape, row_lse is [n_layers][n_q_heads][total_q]."""
     keep, v = _views_like("finch_attend", q, q, cache_k, cache_v, chunk_k, chunk_v, out)
-    shape = q.shape
-    _same_shape("finch_attend: out", out, shape)
+    L, Hq, Hkv, d = _model("finch_attend", ctx, q, q, chunk_k if chunk_k is not None else cache_k)
+    c, shape = batch.c, q.shape
+    rows = c.total_q
+    if shape != (L, Hq, rows, d):
+        _holds("finch_attend: q", shape, (L, Hq, rows, d))
+    if out.shape != shape:
+        _same_shape("finch_attend: out", out, shape)
+    for n, k, value in ((c.total_cache, cache_k, cache_v), (c.total_chunk, chunk_k, chunk_v)):
+        if n and k is not None and value is not None:       # the library refuses what is missing
+            want = L, Hkv, n, d
+            if k.shape != want:
+                _holds("finch_attend: keys", k.shape, want)
+            if value.shape != want:
+                _holds("finch_attend: values", value.shape, want)
+    f32 = _dtypes_of()[1]
+    if batch.q_off.get_device() != q.get_device():
+        raise ValueError(f"finch_attend: the batch description is on {batch.q_off.device}, the tensors on {q.device}")
+    if batch.prompt_self_lse is not None:
+        _rows_of("finch_attend: prompt_self_lse", batch.prompt_self_lse, f32, q, L * Hq * rows, True)
+    if batch.row_limit is not None:
+        _rows_of("finch_attend: row_limit", batch.row_limit, _dtypes_of()[0], q, rows, False)
     z = _VIEW_BYTES
-    _check(load().finch_attend(ctx, v, v + z, v + 2 * z, v + 3 * z, v + 4 * z, C.addressof(batch.c), 1 if causal else 0, v + 5 * z,
-                               _array("finch_attend: row_lse", row_lse, _i32_f32()[1], q, shape[:3]), _ptr(ws), _nbytes(ws),
+    ws, ws_bytes = _space("finch_attend", ws, q)
+    _check(load().finch_attend(ctx, v, v + z, v + 2 * z, v + 3 * z, v + 4 * z, C.addressof(c), 1 if causal else 0, v + 5 * z,
+                               _array("finch_attend: row_lse", row_lse, f32, q, (L, Hq, rows)), ws, ws_bytes,
                                _stream(stream)), "finch_attend")
 
 
@@ -457,6 +521,8 @@ class Pages:
     """The tensors of a paged cache and the finch_pages that describes them."""
     tensors: tuple
     c: finch_pages
+    kind: tuple = ()     # n_layers, n_kv_heads, head_dim, dtype, device index: those of a context
+    requests: int = 0    # rows of the page table
 
 
 def make_pages(k, v, k_scale, v_scale, open_k, open_v, table, open_slot=None) -> Pages:
@@ -476,10 +542,22 @@ def make_pages(k, v, k_scale, v_scale, open_k, open_v, table, open_slot=None) ->
             continue
         if t.dtype != dtype or t.device != k.device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
             raise ValueError(f"make_pages: {name} is to be contiguous {dtype} {tuple(shape)} on {k.device}, got {t.dtype} {tuple(t.shape)}")
+    if open_k.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"make_pages: open rows are float32 or bfloat16, got {open_k.dtype}")
     if page != FINCH_PAGE_TOKENS:
         raise ValueError(f"make_pages: a page has {FINCH_PAGE_TOKENS} tokens, got {page}")
     tensors = (k, v, k_scale, v_scale, open_k, open_v, table, open_slot)
-    return Pages(tensors, finch_pages(*map(_ptr, tensors), n_pages, table.shape[1], n_open))
+    kind = L, Hkv, d, FINCH_F32 if open_k.dtype == torch.float32 else FINCH_BF16, k.get_device()
+    return Pages(tensors, finch_pages(*map(_ptr, tensors), n_pages, table.shape[1], n_open), kind, table.shape[0])
+
+
+def _check_paged(what: str, ctx, pages: Pages, batch: "PagedBatch") -> None:
+    """The pages are of the context's model and device, and their table has the batch's requests."""
+    kind = getattr(ctx, "pages", None)
+    if kind is not None and pages.kind != kind and (pages.kind[:4] != kind[:4] or kind[4] >= 0):
+        raise ValueError(f"{what}: layers, KV heads, head_dim, dtype and device of the pages are {pages.kind}, of the context {kind}")
+    if batch.c.batch > pages.requests or batch.device != pages.kind[4]:
+        raise ValueError(f"{what}: {batch.c.batch} requests on device {batch.device}, a page table of {pages.requests} on {pages.kind[4]}")
 
 
 @dataclass
@@ -489,6 +567,7 @@ class PagedBatch:
     new_off: object
     len: object
     c: finch_paged_batch
+    device: int = -1     # index
 
     @property
     def batch(self) -> int:
@@ -513,20 +592,31 @@ def make_paged_batch(lengths: Sequence[int], q_off: Optional[Sequence[int]] = No
         o = np.ascontiguousarray(off, dtype=np.int32)
         assert len(o) == B + 1
         offs.append((torch.from_numpy(o).to(device), int(o[B]), int(np.diff(o).max()) if B else 0))
+    if any(t is not None and t.get_device() != d_len.get_device() for t, _, _ in offs):
+        raise ValueError(f"make_paged_batch: lengths on {d_len.device}, offsets on {device}")
     longest = (int(h.max()) if B else 0) if max_len is None else int(max_len)
     c = finch_paged_batch(B, _ptr(offs[0][0]), _ptr(offs[1][0]), _ptr(d_len), offs[0][1], offs[1][1], offs[0][2], offs[1][2], longest)
-    return PagedBatch(offs[0][0], offs[1][0], d_len, c)
+    return PagedBatch(offs[0][0], offs[1][0], d_len, c, d_len.get_device())
 
 
 def finch_pages_append(ctx, pages: Pages, batch: PagedBatch, new_k, new_v, out_len=None, rope: Optional[finch_rope] = None, pos=None,
                        stream=None) -> None:
-    """Rows of new_k (turned to their positions with rope) and new_v behind each request's tokens (see the header)."""
-    like = pages.tensors[4]
+    """Rows of new_k (turned to their positions with rope) and new_v, total_new or more, behind each request's tokens (see the header)."""
+    c, kind = batch.c, pages.kind
+    if getattr(ctx, "pages", None) != kind or c.batch > pages.requests or batch.device != kind[4]:
+        _check_paged("finch_pages_append", ctx, pages, batch)
+    like, rows = pages.tensors[4], c.total_new
     keep, v = _views_like("finch_pages_append", like, new_k, new_v)
-    i32 = _i32_f32()[0]
-    _check(load().finch_pages_append(ctx, C.addressof(pages.c), C.addressof(batch.c), v, v + _VIEW_BYTES, _rope(rope),
+    if rows and new_k is not None and new_v is not None:        # the library refuses what is missing
+        want = kind[0], kind[1], rows, kind[2]
+        if new_k.shape != want:
+            _holds("finch_pages_append: new_k", new_k.shape, want)
+        if new_v.shape != want:
+            _holds("finch_pages_append: new_v", new_v.shape, want)
+    i32 = _dtypes_of()[0]
+    _check(load().finch_pages_append(ctx, C.addressof(pages.c), C.addressof(c), v, v + _VIEW_BYTES, _rope(rope),
                                      None if pos is None else _array("finch_pages_append: pos", pos, i32, like, new_k.shape[2:3]),
-                                     _array("finch_pages_append: out_len", out_len, i32, like, (batch.c.batch,)), _stream(stream)),
+                                     _array("finch_pages_append: out_len", out_len, i32, like, (c.batch,)), _stream(stream)),
            "finch_pages_append")
 
 
@@ -537,10 +627,19 @@ def finch_pages_workspace_bytes(ctx, batch: PagedBatch) -> int:
 
 
 def finch_pages_attend(ctx, pages: Pages, batch: PagedBatch, q, out, row_lse=None, ws=None, stream=None) -> None:
-    """Attention of each request's newest tokens over its paged cache (see the header); `out` has q's shape."""
+    """Attention of each request's newest tokens over its paged cache (see the header).  q holds the batch's total_q rows or more;
+    `out` has q's shape, row_lse is [n_layers][n_q_heads][total_q]."""
+    c, kind = batch.c, pages.kind
+    if getattr(ctx, "pages", None) != kind or c.batch > pages.requests or batch.device != kind[4]:
+        _check_paged("finch_pages_attend", ctx, pages, batch)
     keep, v = _views_like("finch_pages_attend", pages.tensors[4], q, out)
-    shape = q.shape
-    _same_shape("finch_pages_attend: out", out, shape)
-    _check(load().finch_pages_attend(ctx, C.addressof(pages.c), C.addressof(batch.c), v, v + _VIEW_BYTES,
-                                     _array("finch_pages_attend: row_lse", row_lse, _i32_f32()[1], q, shape[:3]), _ptr(ws),
-                                     _nbytes(ws), _stream(stream)), "finch_pages_attend")
+    rows, shape, m = c.total_q, q.shape, getattr(ctx, "model", None)
+    L, Hq = kind[0], m[1] if m is not None else shape[1]
+    if shape != (L, Hq, rows, kind[2]):
+        _holds("finch_pages_attend: q", shape, (L, Hq, rows, kind[2]))
+    if out.shape != shape:
+        _same_shape("finch_pages_attend: out", out, shape)
+    ws, ws_bytes = _space("finch_pages_attend", ws, q)
+    _check(load().finch_pages_attend(ctx, C.addressof(pages.c), C.addressof(c), v, v + _VIEW_BYTES,
+                                     _array("finch_pages_attend: row_lse", row_lse, _dtypes_of()[1], q, (L, Hq, rows)), ws, ws_bytes,
+                                     _stream(stream)), "finch_pages_attend")

@@ -294,3 +294,73 @@ def test_a_cache_checks_the_document_that_fills_it(monkeypatch):
     with pytest.raises(RuntimeError):
         cache.fill(Refused())
     assert not moved and cache.len.tolist() == [0]
+
+
+def test_the_binding_refuses_tensors_that_do_not_hold_the_call(lib, ctx, monkeypatch):
+    """A call takes addresses and strides; rows, heads and layers are the context's and the batch's.  A tensor that has fewer would be read
+    and written behind its end, one of another type misread.  (The context has 2 layers, 8 and 2 heads of 64, bf16.)"""
+    import torch
+    monkeypatch.setattr(fb, "_stream", lambda stream: None)
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)
+
+    def refused(call, base, **changes):
+        with pytest.raises(fb.FinchError) as e:          # as it is, a call stops at the launch
+            call(ctx, **base)
+        assert e.value.status == UNSUPPORTED
+        for name, value in changes.items():
+            for v in value:
+                a = dict(base)
+                for n, x in (v.items() if isinstance(v, dict) else [(name, v)]):
+                    a[n] = x
+                with pytest.raises(ValueError):
+                    call(ctx, **a)
+
+    q, k = bf(2, 8, 5, 64), bf(2, 2, 5, 64)
+    refused(fb.finch_rotate, dict(q=q, k=k, pos=i32(1, 2, 3, 4, 5), out_q=bf(2, 8, 5, 64), out_k=bf(2, 2, 5, 64), rope=rope()),
+            heads=[dict(q=bf(2, 4, 5, 64), out_q=bf(2, 4, 5, 64)), dict(k=bf(2, 1, 5, 64), out_k=bf(2, 1, 5, 64)),
+                   dict(q=None, out_q=None, k=bf(2, 1, 5, 64), out_k=bf(2, 1, 5, 64))],
+            layers=[dict(q=bf(1, 8, 5, 64), k=bf(1, 2, 5, 64), out_q=bf(1, 8, 5, 64), out_k=bf(1, 2, 5, 64))],
+            dim=[dict(q=bf(2, 8, 5, 32), k=bf(2, 2, 5, 32), out_q=bf(2, 8, 5, 32), out_k=bf(2, 2, 5, 32))],
+            dtype=[{n: x.float() for n, x in (("q", q), ("k", k), ("out_q", q), ("out_k", k))}],
+            rank=[dict(q=bf(8), out_q=bf(8))])
+
+    batch = fb.make_batch([0, 5], [0, 6], [0, 7], [7], [7], device="cpu")
+    rows = fb.make_batch([0, 6], [0, 6], [0, 7], [7], [7], device="cpu")
+    limited = lambda **kw: fb.make_batch([0, 5], [0, 6], [0, 7], [7], [7], device="cpu", **kw)
+    space = torch.zeros(1 << 22, dtype=torch.uint8)
+    attend = dict(q=q, cache_k=bf(2, 2, 7, 64), cache_v=bf(2, 2, 7, 64), chunk_k=bf(2, 2, 6, 64), chunk_v=bf(2, 2, 6, 64), batch=batch,
+                  out=bf(2, 8, 5, 64), row_lse=torch.zeros(2, 8, 5), ws=space)
+    refused(fb.finch_attend, attend, batch=[rows, limited(prompt_self_lse=torch.zeros(2, 8, 4)), limited(prompt_self_lse=torch.zeros(2, 8, 6)),
+                                            limited(prompt_self_lse=torch.zeros(2, 8, 5).double()), limited(row_limit=i32(1, 2, 3, 4)),
+                                            limited(row_limit=i32(1, 2, 3, 4, 5).long())],
+            cache_k=[bf(2, 2, 6, 64), bf(2, 1, 7, 64), bf(1, 2, 7, 64)], cache_v=[bf(2, 2, 6, 64)], chunk_k=[bf(2, 2, 5, 64), bf(2, 2, 6, 32)],
+            chunk_v=[bf(2, 2, 5, 64)], ws=[torch.zeros((1 << 22, 2), dtype=torch.uint8)[:, 0]],
+            heads=[dict(q=bf(2, 4, 5, 64), out=bf(2, 4, 5, 64), row_lse=None)])
+    # more rows than the batch's are a padded batch; row_lse then has the batch's
+    padded = dict(attend, q=bf(2, 8, 9, 64), out=bf(2, 8, 9, 64), cache_k=bf(2, 2, 9, 64), chunk_v=bf(2, 2, 8, 64))
+    refused(fb.finch_attend, padded, row_lse=[torch.zeros(2, 8, 9)])
+    refused(fb.finch_attend, dict(attend, batch=limited(prompt_self_lse=torch.zeros(2, 8, 5), row_limit=i32(1, 2, 3, 4, 5, 6))))
+
+    def pages(L=2, Hkv=2, d=64, requests=2, dtype=torch.bfloat16):
+        pool, scale = (lambda: torch.zeros((L, 3, Hkv, 64, d), dtype=torch.uint8)), (lambda: torch.zeros((L, 3, Hkv)))
+        rows = lambda: torch.zeros((L, 2, Hkv, 64, d), dtype=dtype)
+        return fb.make_pages(pool(), pool(), scale(), scale(), rows(), rows(), torch.zeros((requests, 3), dtype=torch.int32))
+
+    two = fb.make_paged_batch([10, 3], q_off=[0, 2, 5], new_off=[0, 2, 5], device="cpu")
+    six = fb.make_paged_batch([10, 3], q_off=[0, 2, 6], new_off=[0, 2, 6], device="cpu")
+    other = [pages(L=1), pages(Hkv=1), pages(d=32), pages(requests=1), pages(dtype=torch.float32)]
+    refused(fb.finch_pages_append, dict(pages=pages(), batch=two, new_k=k, new_v=k), pages=other, batch=[six],
+            new_k=[bf(2, 2, 4, 64), bf(2, 1, 5, 64), bf(1, 2, 5, 64)], new_v=[bf(2, 2, 4, 64), bf(2, 2, 5, 32)])
+    decode = dict(pages=pages(), batch=two, q=q, out=bf(2, 8, 5, 64), row_lse=torch.zeros(2, 8, 5), ws=space)
+    refused(fb.finch_pages_attend, decode, pages=other, batch=[six], heads=[dict(q=bf(2, 4, 5, 64), out=bf(2, 4, 5, 64), row_lse=None)],
+            ws=[torch.zeros((1 << 22, 2), dtype=torch.uint8)[:, 0]])
+    refused(fb.finch_pages_attend, dict(decode, q=bf(2, 8, 7, 64), out=bf(2, 8, 7, 64)), row_lse=[torch.zeros(2, 8, 7)])
+    with pytest.raises(ValueError):
+        pages(dtype=torch.float16)
+    # a handle from elsewhere: the tensors among themselves
+    raw = C.c_void_p(ctx.value)
+    with pytest.raises(ValueError):
+        fb.finch_attend(raw, **dict(attend, cache_v=bf(2, 1, 7, 64)))
+    with pytest.raises(ValueError):
+        fb.finch_pages_append(raw, pages(Hkv=1), two, k, k)
