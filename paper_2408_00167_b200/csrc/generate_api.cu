@@ -183,6 +183,12 @@ finch_status finch_attend(finch_ctx *ctx, const finch_tensor *q, const finch_ten
         if (views_overlap(ctx, out, batch->total_q, ctx->model.Hq, ins[i], i < 2 ? batch->total_cache : batch->total_chunk, ctx->model.Hkv))
             return FINCH_ERR_INVALID_ARG;
     if (views_overlap(ctx, out, batch->total_q, ctx->model.Hq, q, batch->total_q, ctx->model.Hq)) return FINCH_ERR_INVALID_ARG;
+    // the CTAs (and warps) that share a row read its extra term, and one of them writes its row_lse
+    if (row_lse && batch->prompt_self_lse) {
+        const uintptr_t a = (uintptr_t)row_lse, n = (uintptr_t)batch->prompt_self_lse;
+        const uintptr_t bytes = (uintptr_t)ctx->model.L * ctx->model.Hq * batch->total_q * sizeof(float);
+        if (a < n + bytes && n < a + bytes) return FINCH_ERR_INVALID_ARG;
+    }
     if (!ws) return FINCH_ERR_INVALID_ARG;
     if (!aligned16(ws)) return FINCH_ERR_BAD_LAYOUT;
     const AttendWs w = attend_ws(ctx, batch->total_q);

@@ -364,3 +364,17 @@ def test_the_binding_refuses_tensors_that_do_not_hold_the_call(lib, ctx, monkeyp
         fb.finch_attend(raw, **dict(attend, cache_v=bf(2, 1, 7, 64)))
     with pytest.raises(ValueError):
         fb.finch_pages_append(raw, pages(Hkv=1), two, k, k)
+
+
+def test_attend_refuses_log_sum_exps_over_the_extra_term(lib, ctx):
+    """Several warps and CTAs read a row's extra term while one of them writes its log-sum-exp."""
+    b, far = _batch(q=40), 0x2000_0000
+    b.prompt_self_lse = BASE + far
+    tensors = [tensor(0, 40, 8), tensor(1, 70, 2), tensor(2, 70, 2), tensor(3, 90, 2), tensor(4, 90, 2)]
+    out, size = tensor(5, 40, 8), 2 * 8 * 40 * 4
+    call = lambda lse: lib.finch_attend(ctx, *map(C.addressof, tensors), C.addressof(b), 1, C.addressof(out), lse, BASE, 1 << 40, None)
+    for at in (0, 4, size - 4, 4 - size):
+        assert call(BASE + far + at) == INVALID
+    for at in (size, -size):
+        assert call(BASE + far + at) == UNSUPPORTED               # valid: stops at the launch
+    assert call(None) == UNSUPPORTED
