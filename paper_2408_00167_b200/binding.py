@@ -184,6 +184,13 @@ def _stream(stream) -> Optional[int]:
     return _current_stream() or None
 
 
+def device_of(device):
+    """The torch.device with its index: "cuda" alone is the device that is current now, and what is made later belongs beside it."""
+    import torch
+    device = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
+
+
 @dataclass
 class Batch:
     """Device-side batch metadata plus the host bounds finch_batch carries."""

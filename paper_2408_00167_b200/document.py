@@ -47,7 +47,7 @@ class DocumentCompressor:
                  scale: float = 0.0, rope_theta: float = 0.0, rope_pairing: int = 0, device="cuda"):
         import torch
         self.torch = torch
-        self.device = device
+        self.device = device = fb.device_of(device)
         self.L, self.Hq, self.Hkv, self.d = n_layers, n_q_heads, n_kv_heads, head_dim
         self.G = n_kv_heads if group_mode == fb.FINCH_GROUP_PER_KV_HEAD else 1
         self.capacity = np.asarray(capacity, dtype=np.int32)
@@ -58,7 +58,7 @@ class DocumentCompressor:
         self.ctx = fb.finch_ctx_create(n_layers, n_q_heads, n_kv_heads, head_dim, dtype, group_mode, scale,
                                        max_batch=max(self.B, 1), max_prompt=max(max_prompt, 1),
                                        max_candidates=max(int(self.capacity.max(initial=0)) + max_chunk, 1),
-                                       device=torch.device(device).index or 0, rope_theta=rope_theta,
+                                       device=device.index or 0, rope_theta=rope_theta,
                                        rope_pairing=rope_pairing)
         mk = lambda: dict(k=torch.zeros((n_layers, n_kv_heads, total_cap, head_dim), dtype=tdtype, device=device),
                           v=torch.zeros((n_layers, n_kv_heads, total_cap, head_dim), dtype=tdtype, device=device),

@@ -35,7 +35,8 @@ class PagedCache:
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, batch: int, max_tokens: int,
                  max_step: int = 1, scale: float = 0.0, rope: Optional[fb.finch_rope] = None, device="cuda"):
         import torch
-        self.torch, self.device, self.rope = torch, device, rope
+        self.torch, self.device, self.rope = torch, fb.device_of(device), rope
+        device = self.device
         self.L, self.Hq, self.Hkv, self.d, self.B = n_layers, n_q_heads, n_kv_heads, head_dim, batch
         self.max_tokens, self.max_step = max_tokens, max(max_step, 1)
         width = -(-max_tokens // fb.FINCH_PAGE_TOKENS)
@@ -50,8 +51,7 @@ class PagedCache:
         self.pages = fb.make_pages(*self._tensors, self.table, self.slot)
         # a layer's calls see that layer's part of every array
         self._of_layer = [fb.make_pages(*(t[l:l + 1] for t in self._tensors), self.table, self.slot) for l in range(n_layers)]
-        index = torch.device(device).index or 0
-        bounds = dict(max_batch=max(batch, 1), max_prompt=self.max_step, max_candidates=max(max_tokens, 1), device=index)
+        bounds = dict(max_batch=max(batch, 1), max_prompt=self.max_step, max_candidates=max(max_tokens, 1), device=device.index or 0)
         self._ctx_all = fb.finch_ctx_create(n_layers, n_q_heads, n_kv_heads, head_dim, dtype, scale=scale, **bounds)
         self._ctx = fb.finch_ctx_create(1, n_q_heads, n_kv_heads, head_dim, dtype, scale=scale, **bounds)
         self.len = np.zeros(batch, dtype=np.int32)

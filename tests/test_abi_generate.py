@@ -378,3 +378,30 @@ def test_attend_refuses_log_sum_exps_over_the_extra_term(lib, ctx):
     for at in (size, -size):
         assert call(BASE + far + at) == UNSUPPORTED               # valid: stops at the launch
     assert call(None) == UNSUPPORTED
+
+
+def test_holders_stay_on_the_device_that_was_current(lib, monkeypatch):
+    """device="cuda" is the device that is current when the object is made, for its contexts, its tensors and what later steps upload."""
+    import torch
+    from paper_2408_00167_b200.document import DocumentCompressor
+    from paper_2408_00167_b200.generate import PagedCache
+    current, seen, create = [3], [], fb.finch_ctx_create
+
+    def on_cpu(name):
+        real = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, device=None, **kw: (seen.append(device), real(*a, **kw))[1])
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(fb, "finch_ctx_create", lambda *a, **kw: (seen.append(torch.device("cuda", kw["device"])), create(*a, **{**kw, "device": -1}))[1])
+    for name in ("zeros", "full", "arange", "empty"):
+        on_cpu(name)
+    sizes = dict(n_layers=1, n_q_heads=2, n_kv_heads=1, head_dim=64, dtype=fb.FINCH_BF16)
+    for make in (lambda **kw: PagedCache(batch=2, max_tokens=100, **sizes, **kw),
+                 lambda **kw: DocumentCompressor(capacity=[8], max_prompt=4, max_chunk=4, **sizes, **kw)):
+        for kw, want in ((dict(), "cuda:3"), (dict(device="cuda"), "cuda:3"), (dict(device="cuda:1"), "cuda:1"), (dict(device=torch.device("cuda", 0)), "cuda:0")):
+            seen.clear()
+            held = make(**kw)
+            current[0] = 5
+            assert seen and set(map(str, seen)) == {want} and str(held.device) == want
+            current[0] = 3
+            held.close()
