@@ -56,6 +56,7 @@ class PagedCache:
         self._ctx = fb.finch_ctx_create(1, n_q_heads, n_kv_heads, head_dim, dtype, scale=scale, **bounds)
         self.len = np.zeros(batch, dtype=np.int32)
         self._add = self._see = self._ws = None
+        self._steps, self._has = 0, [0] * n_layers      # steps since the cache was filled, and those whose rows a layer has
 
     def close(self) -> None:
         for name in ("_ctx", "_ctx_all"):
@@ -86,6 +87,7 @@ class PagedCache:
             fb.finch_pages_append(self._ctx_all, one, batch, doc.cache_k[:, :, at:at + n], doc.cache_v[:, :, at:at + n])
         self.len = doc.cache_len.astype(np.int32).copy()
         self._add = self._see = None
+        self._steps, self._has = 0, [0] * self.L
 
     def step(self, tokens: int = 1) -> None:
         """`tokens` more of every request: appends and attention of all layers follow, then the next step."""
@@ -97,6 +99,7 @@ class PagedCache:
         self._add = fb.make_paged_batch(self.len, new_off=off, device=self.device)
         self.len = self.len + np.int32(tokens)
         self._see = fb.make_paged_batch(self.len, q_off=off, device=self.device)
+        self._steps += 1
         if self._ws is None:
             self._ws = self.torch.empty(fb.finch_pages_workspace_bytes(self._ctx, self._see), dtype=self.torch.uint8, device=self.device)
 
@@ -105,16 +108,23 @@ class PagedCache:
             raise ValueError(f"PagedCache.{what}: expected rows {(1, heads, self._add.c.total_new, self.d)}, got {tuple(t.shape)}")
 
     def append(self, layer: int, k, v) -> None:
-        """The step's new rows of a layer, [1][n_kv_heads][batch * tokens][head_dim], requests one behind the other."""
+        """The step's new rows of a layer, [1][n_kv_heads][batch * tokens][head_dim], requests one behind the other; once a step (a
+        second time open rows would be read that the first has moved on)."""
         if self._add is None:
             raise ValueError("PagedCache.append: no step has been begun")
+        if self._has[layer] != self._steps - 1:
+            raise ValueError(f"PagedCache.append: layer {layer} has the rows of {self._has[layer]} steps, this is step {self._steps}")
         self._check_rows("append", k, self.Hkv)
         self._check_rows("append", v, self.Hkv)
         fb.finch_pages_append(self._ctx, self._of_layer[layer], self._add, k, v, rope=self.rope)
+        self._has[layer] = self._steps
 
     def attend(self, layer: int, q, out, row_lse=None) -> None:
-        """Attention of the step's query rows, [1][n_q_heads][batch * tokens][head_dim], over the layer's cache."""
+        """Attention of the step's query rows, [1][n_q_heads][batch * tokens][head_dim], over the layer's cache, the step's rows among
+        it."""
         if self._see is None:
             raise ValueError("PagedCache.attend: no step has been begun")
+        if self._has[layer] != self._steps:
+            raise ValueError(f"PagedCache.attend: layer {layer} has the rows of {self._has[layer]} steps, this is step {self._steps}")
         self._check_rows("attend", q, self.Hq)
         fb.finch_pages_attend(self._ctx, self._of_layer[layer], self._see, q, out, row_lse, ws=self._ws)

@@ -405,3 +405,43 @@ def test_holders_stay_on_the_device_that_was_current(lib, monkeypatch):
             assert seen and set(map(str, seen)) == {want} and str(held.device) == want
             current[0] = 3
             held.close()
+
+
+def test_a_layer_gets_the_rows_of_every_step_once(lib, monkeypatch):
+    """What append and attend of a PagedCache would get wrong: a layer twice in a step, attention before the step's rows are there, a
+    layer that missed a step.  A layer that is never used does no harm."""
+    import torch
+    from paper_2408_00167_b200.generate import PagedCache
+    create, calls = fb.finch_ctx_create, []
+    monkeypatch.setattr(fb, "finch_ctx_create", lambda *a, **kw: create(*a, **{**kw, "device": -1}))
+    monkeypatch.setattr(fb, "finch_pages_append", lambda *a, **kw: calls.append("append"))
+    monkeypatch.setattr(fb, "finch_pages_attend", lambda *a, **kw: calls.append("attend"))
+    cache = PagedCache(3, 2, 1, 64, fb.FINCH_F32, 2, max_tokens=70, max_step=2, device="cpu")
+    k = lambda n: torch.zeros((1, 1, 2 * n, 64))
+    q = lambda n: torch.zeros((1, 2, 2 * n, 64))
+
+    def refused(call, *args):
+        n = len(calls)
+        with pytest.raises(ValueError):
+            call(*args)
+        assert len(calls) == n
+
+    cache.step()
+    refused(cache.attend, 0, q(1), q(1))
+    cache.append(0, k(1), k(1))
+    cache.attend(0, q(1), q(1))
+    cache.attend(0, q(1), q(1))
+    refused(cache.append, 0, k(1), k(1))
+    refused(cache.attend, 1, q(1), q(1))
+    cache.append(-2, k(1), k(1))                 # layer 1
+    refused(cache.append, 1, k(1), k(1))
+    cache.step(2)
+    cache.append(0, k(2), k(2))
+    refused(cache.attend, 1, q(2), q(2))
+    refused(cache.append, 2, k(2), k(2))         # it has missed a step
+    refused(cache.attend, 2, q(2), q(2))
+    cache.append(1, k(2), k(2))
+    cache.attend(1, q(2), q(2))
+    refused(cache.append, 1, k(2), k(2))
+    assert calls == ["append", "attend", "attend", "append", "append", "append", "attend"] and cache.len.tolist() == [3, 3]
+    cache.close()
