@@ -56,6 +56,7 @@ class PagedCache:
         self._ctx = fb.finch_ctx_create(1, n_q_heads, n_kv_heads, head_dim, dtype, scale=scale, **bounds)
         self.len = np.zeros(batch, dtype=np.int32)
         self._add = self._see = self._ws = None
+        self._made_on = self._step_on = self._stream()   # the streams that the arrays above and a step's description belong to
         self._steps, self._has = 0, [0] * n_layers      # steps since the cache was filled, and those whose rows a layer has
 
     def close(self) -> None:
@@ -84,6 +85,7 @@ class PagedCache:
             n, at = int(doc.cache_len[b]), int(doc.cache_off[b])
             one = fb.make_pages(*self._tensors, self.table[b:b + 1], self.slot[b:b + 1])
             batch = fb.make_paged_batch([0], new_off=[0, n], device=self.device)
+            self._read_here(batch, self._stream())
             fb.finch_pages_append(self._ctx_all, one, batch, doc.cache_k[:, :, at:at + n], doc.cache_v[:, :, at:at + n])
         self.len = doc.cache_len.astype(np.int32).copy()
         self._add = self._see = None
@@ -96,12 +98,26 @@ class PagedCache:
         if int(self.len.max(initial=0)) + tokens > self.max_tokens:
             raise ValueError(f"PagedCache.step: room for {self.max_tokens} tokens")
         off = np.arange(self.B + 1, dtype=np.int32) * tokens
+        self._step_on = self._stream()
         self._add = fb.make_paged_batch(self.len, new_off=off, device=self.device)
         self.len = self.len + np.int32(tokens)
         self._see = fb.make_paged_batch(self.len, q_off=off, device=self.device)
         self._steps += 1
         if self._ws is None:
             self._ws = self.torch.empty(fb.finch_pages_workspace_bytes(self._ctx, self._see), dtype=self.torch.uint8, device=self.device)
+
+    def _stream(self):
+        return fb._stream(None) if self.device.type == "cuda" else None
+
+    def _read_here(self, batch, made_on) -> None:
+        """A step's description is replaced by the next one's, and everything goes when the cache does: memory that the current stream's
+        kernels read, where it was allocated for another stream, waits for them before it serves another purpose."""
+        if self._stream() == made_on == self._made_on:
+            return
+        stream = self.torch.cuda.current_stream()
+        for t in (*self._tensors, self.table, self.slot, self._ws, batch.q_off, batch.new_off, batch.len):
+            if t is not None:
+                t.record_stream(stream)
 
     def _check_rows(self, what: str, t, heads: int) -> None:
         if t.shape != (1, heads, self._add.c.total_new, self.d):
@@ -116,6 +132,7 @@ class PagedCache:
             raise ValueError(f"PagedCache.append: layer {layer} has the rows of {self._has[layer]} steps, this is step {self._steps}")
         self._check_rows("append", k, self.Hkv)
         self._check_rows("append", v, self.Hkv)
+        self._read_here(self._add, self._step_on)
         fb.finch_pages_append(self._ctx, self._of_layer[layer], self._add, k, v, rope=self.rope)
         self._has[layer] = self._steps
 
@@ -127,4 +144,5 @@ class PagedCache:
         if self._has[layer] != self._steps:
             raise ValueError(f"PagedCache.attend: layer {layer} has the rows of {self._has[layer]} steps, this is step {self._steps}")
         self._check_rows("attend", q, self.Hq)
+        self._read_here(self._see, self._step_on)
         fb.finch_pages_attend(self._ctx, self._of_layer[layer], self._see, q, out, row_lse, ws=self._ws)

@@ -392,6 +392,7 @@ def test_holders_stay_on_the_device_that_was_current(lib, monkeypatch):
         monkeypatch.setattr(torch, name, lambda *a, device=None, **kw: (seen.append(device), real(*a, **kw))[1])
 
     monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(fb, "_stream", lambda stream: None)
     monkeypatch.setattr(fb, "finch_ctx_create", lambda *a, **kw: (seen.append(torch.device("cuda", kw["device"])), create(*a, **{**kw, "device": -1}))[1])
     for name in ("zeros", "full", "arange", "empty"):
         on_cpu(name)
@@ -444,4 +445,36 @@ def test_a_layer_gets_the_rows_of_every_step_once(lib, monkeypatch):
     cache.attend(1, q(2), q(2))
     refused(cache.append, 1, k(2), k(2))
     assert calls == ["append", "attend", "attend", "append", "append", "append", "attend"] and cache.len.tolist() == [3, 3]
+    cache.close()
+
+
+def test_a_cache_keeps_what_another_stream_reads(lib, monkeypatch):
+    """A step's description made on one stream and read on another is held for that one (nothing is held where they are the same)."""
+    import torch
+    from paper_2408_00167_b200.generate import PagedCache
+    create, now, held = fb.finch_ctx_create, ["a"], []
+    monkeypatch.setattr(fb, "finch_ctx_create", lambda *a, **kw: create(*a, **{**kw, "device": -1}))
+    for name in ("finch_pages_append", "finch_pages_attend"):
+        monkeypatch.setattr(fb, name, lambda *a, **kw: None)
+    monkeypatch.setattr(PagedCache, "_stream", lambda self: now[0])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: now[0])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: held.append((self.data_ptr(), s)))
+    cache = PagedCache(1, 2, 1, 64, fb.FINCH_F32, 2, max_tokens=70, device="cpu")
+    k, q = torch.zeros((1, 1, 2, 64)), torch.zeros((1, 2, 2, 64))
+
+    def both():
+        held.clear()
+        cache.append(0, k, k)
+        cache.attend(0, q, q)
+        return held
+
+    cache.step()
+    assert not both()
+    for made, read in (("a", "b"), ("b", "a"), ("b", "b")):
+        now[0] = made
+        cache.step()
+        now[0] = read
+        pointers = {p for p, s in both() if s == read}
+        for t in (cache._add.new_off, cache._add.len, cache._see.q_off, cache._see.len, cache._ws, cache.table, *cache._tensors):
+            assert t.data_ptr() in pointers
     cache.close()

@@ -163,3 +163,31 @@ def test_a_document_whose_step_was_refused_does_not_become_a_cache():
     finally:
         cache.close()
         doc.close()
+
+
+def test_steps_on_one_stream_and_calls_on_another():
+    """Descriptions of steps are made on the current stream; a slow other stream still reads those of steps long past."""
+    import torch
+    Hq, Hkv, d, B, steps = 4, 2, 64, 3, 40
+    g = torch.Generator(device="cuda").manual_seed(7)
+    rows = [[torch.randn((1, h, B, d), generator=g, device="cuda") for h in (Hkv, Hkv, Hq)] for _ in range(steps)]
+    side, results = torch.cuda.Stream(), []
+    for other in (False, True):
+        cache = PagedCache(1, Hq, Hkv, d, fb.FINCH_F32, B, max_tokens=steps)
+        out = [torch.full_like(q, math.nan) for _, _, q in rows]
+        torch.cuda.synchronize()
+        stream = side if other else torch.cuda.current_stream()
+        if other:
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(200_000_000)      # some 0.1 s, in which all steps are made
+        for (k, v, q), o in zip(rows, out):
+            cache.step()
+            with torch.cuda.stream(stream):
+                cache.append(0, k, v)
+                cache.attend(0, q, o)
+            torch.full((B,), 1, dtype=torch.int32, device="cuda")     # takes memory of the sizes that a step's arrays have
+        torch.cuda.synchronize()
+        assert cache.status() == 0
+        results.append(out)
+        cache.close()
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and not any(torch.isnan(a).any() for a in results[0])
