@@ -333,6 +333,19 @@ finch_status finch_attend(finch_ctx *ctx, const finch_tensor *q, const finch_ten
                           const finch_tensor *chunk_k, const finch_tensor *chunk_v, const finch_batch *batch, int32_t causal,
                           const finch_tensor *out, float *row_lse, void *ws, size_t ws_bytes, void *cuda_stream);
 
+/* How finch_attend's kernels share out a batch (given a workspace of finch_attend_workspace_bytes).  Host arithmetic on the batch's
+ * bounds, nothing is enqueued, works on a validation-only context (then for 148 SMs).
+ *  - FINCH_ATTEND_MULTIPLY_ADD: fp32 inputs or head_dim above 128.
+ *  - FINCH_ATTEND_ONE_STREAM: a CTA has one tile of 128 rows, two CTAs share an SM.
+ *  - FINCH_ATTEND_ROW_PAIRS: a CTA has two row tiles against the same keys.
+ *  - FINCH_ATTEND_KEY_PAIRS: a CTA has one row tile against its even and its odd key tiles.
+ * *cluster receives the CTAs of a cluster that share a row's keys, *splits how often a row's keys are split beyond that (the parts are
+ * added by a second launch); both may be NULL.  A batch whose tensors the TMA unit cannot describe (an outer stride of zero, or of
+ * 2^40 bytes or more) takes the multiply-adds regardless; that depends on the tensors and is not reported here.
+ * Errors: as finch_attend_workspace_bytes. */
+enum { FINCH_ATTEND_MULTIPLY_ADD = 0, FINCH_ATTEND_ONE_STREAM = 1, FINCH_ATTEND_ROW_PAIRS = 2, FINCH_ATTEND_KEY_PAIRS = 3 };
+finch_status finch_attend_plan(const finch_ctx *ctx, const finch_batch *batch, int32_t *path, int32_t *cluster, int32_t *splits);
+
 /* A paged cache in 8 bits.  Token t of request b lies in page table[b][t / 64], row t % 64, once that page is full: e4m3 codes with one
  * scale for each page and KV head (value = code * scale, scale = largest finite magnitude / 448).  The tokens behind the last full page wait in
  * the open rows of the request's slot, in the context's dtype: a page is quantised once, from unrounded rows, however they arrived.

@@ -35,7 +35,7 @@ FINCH_DEV_BAD_BATCH, FINCH_DEV_TIMEOUT, FINCH_DEV_BAD_INDEX = 1, 2, 4
 EXPORTS = ("finch_ctx_create", "finch_ctx_destroy", "finch_workspace_bytes", "finch_score", "finch_select",
            "finch_compact", "finch_step", "finch_device_status", "finch_launch_count", "finch_status_string", "finch_score_static", "finch_score_static_max_rows", "finch_score_static_path",
            "finch_step_host", "finch_score_plan", "finch_rope_frequencies", "finch_rope_init", "finch_rotate",
-           "finch_attend_workspace_bytes", "finch_attend", "finch_pages_append", "finch_pages_workspace_bytes", "finch_pages_attend")
+           "finch_attend_workspace_bytes", "finch_attend_plan", "finch_attend", "finch_pages_append", "finch_pages_workspace_bytes", "finch_pages_attend")
 
 
 class finch_config(C.Structure):
@@ -111,6 +111,7 @@ def load() -> C.CDLL:
         lib.finch_rope_init.argtypes = [p, i, i, f, p]
         lib.finch_rotate.argtypes = [p, p, p, i, p, p, p, p, f, p, p, p]
         lib.finch_attend_workspace_bytes.argtypes = [p] * 3
+        lib.finch_attend_plan.argtypes = [p] * 5
         lib.finch_attend.argtypes = [p] * 7 + [i, p, p, p, z, p]
         lib.finch_pages_append.argtypes = [p] * 9
         lib.finch_pages_workspace_bytes.argtypes = [p] * 3
@@ -488,6 +489,16 @@ def finch_attend_workspace_bytes(ctx, batch: Batch) -> int:
     out = C.c_size_t()
     _check(load().finch_attend_workspace_bytes(ctx, C.addressof(batch.c), C.addressof(out)), "finch_attend_workspace_bytes")
     return int(out.value)
+
+
+FINCH_ATTEND_MULTIPLY_ADD, FINCH_ATTEND_ONE_STREAM, FINCH_ATTEND_ROW_PAIRS, FINCH_ATTEND_KEY_PAIRS = 0, 1, 2, 3
+
+
+def finch_attend_plan(ctx, batch: Batch):
+    """(path, cluster, splits): how finch_attend shares out this batch (see the header)."""
+    out = [C.c_int32() for _ in range(3)]
+    _check(load().finch_attend_plan(ctx, C.addressof(batch.c), *map(C.addressof, out)), "finch_attend_plan")
+    return tuple(x.value for x in out)
 
 
 def finch_attend(ctx, q, cache_k, cache_v, chunk_k, chunk_v, batch: Batch, out, row_lse=None, causal: bool = True, ws=None,

@@ -82,6 +82,9 @@ constexpr int kAttendSimtRows = 64;   // .. of the warp-level path
 constexpr int kPagesRows = 8;         // .. of the paged path
 
 bool attend_tc_supported(const Ctx &ctx);
+// what the launches below make of a batch's bounds (FINCH_ATTEND_..)
+void attend_tc_plan(const Ctx &ctx, const BatchView &bv, size_t partial_rows, int &path, int &cluster, int &clusters);
+int attend_simt_splits(const Ctx &ctx, const BatchView &bv, size_t partial_rows);
 cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorView &ck, const TensorView &cv, const TensorView &hk,
                              const TensorView &hv, const BatchView &bv, int causal, AttendOut out, size_t partial_rows, cudaStream_t stream);
 cudaError_t launch_attend_simt(const Ctx &ctx, const TensorView &q, const TensorView &ck, const TensorView &cv, const TensorView &hk,

@@ -273,39 +273,53 @@ cudaError_t launch_t(const Ctx &ctx, const SimtArgs &p, int rows, dim3 grid, cud
     return rows == 32 ? launch_d<T, 32>(ctx, p, grid, stream) : launch_d<T, 64>(ctx, p, grid, stream);
 }
 
+struct Plan {
+    int per_cta, heads, tok, chunks, row_tiles, splits;
+};
+
+// Host arithmetic on the batch's bounds; partial_rows: rows of partial results that there is place for.
+Plan make_plan(const Ctx &ctx, const BatchView &bv, size_t partial_rows) {
+    const ModelView &mv = ctx.model;
+    const int sms = ctx.sm_count > 0 ? ctx.sm_count : 148;   // a validation-only context has none
+    Plan n;
+    // 64 rows to a CTA, fewer where there are no more, or where that leaves most SMs without one and the keys are few (8 heads of 64: 16 rows
+    // over 16 8.9 us with 64, 5.4 with 16; 256 over 256 19.0, 14.7 with 32, 16.8 with 16; 512 over 512 29, 35, 38; 100 over 2148 35, 43, 65)
+    const int key_tiles = (bv.max_cache + kK - 1) / kK + (bv.max_chunk + kK - 1) / kK;
+    int64_t units = 0, tiles = 0;
+    for (n.per_cta = kAttendSimtRows;; n.per_cta /= 2) {
+        // as many heads as share their keys, at least one token
+        n.heads = mv.g < n.per_cta ? mv.g : n.per_cta;
+        n.tok = n.per_cta / n.heads;
+        n.chunks = (mv.g + n.heads - 1) / n.heads;
+        tiles = (bv.max_q + n.tok - 1) / n.tok;
+        units = (int64_t)mv.L * mv.Hkv * n.chunks;
+        const bool fits = (int64_t)bv.max_q * mv.g * 2 <= n.per_cta, idle = key_tiles <= 4 && units * tiles * bv.batch < sms / 4;
+        if (n.per_cta == 16 || !(fits || idle)) break;
+    }
+    n.row_tiles = (int)tiles;
+    const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
+    n.splits = attend_splits(units * tiles * bv.batch, sms, key_tiles, 2);
+    while (n.splits > 1 && n.splits * rows > partial_rows) --n.splits;
+    return n;
+}
+
 }  // namespace
+
+int attend_simt_splits(const Ctx &ctx, const BatchView &bv, size_t partial_rows) { return make_plan(ctx, bv, partial_rows).splits; }
 
 cudaError_t launch_attend_simt(const Ctx &ctx, const TensorView &q, const TensorView &ck, const TensorView &cv, const TensorView &hk,
                                const TensorView &hv, const BatchView &bv, int causal, AttendOut out, size_t partial_rows,
                                cudaStream_t stream) {
     if (bv.batch == 0 || bv.max_q == 0) return cudaSuccess;
     const ModelView &mv = ctx.model;
-    SimtArgs p = {mv, bv, q, ck, cv, hk, hv, out, ctx.d_status, causal, 0, 0, 0, 0, mv.scale * kLog2e};
-    // 64 rows to a CTA, fewer where there are no more, or where that leaves most SMs without one and the keys are few (8 heads of 64: 16 rows
-    // over 16 8.9 us with 64, 5.4 with 16; 256 over 256 19.0, 14.7 with 32, 16.8 with 16; 512 over 512 29, 35, 38; 100 over 2148 35, 43, 65)
-    const int key_tiles = (bv.max_cache + kK - 1) / kK + (bv.max_chunk + kK - 1) / kK;
-    int64_t units = 0, tiles = 0;
-    int per_cta = kAttendSimtRows;
-    for (;; per_cta /= 2) {
-        // as many heads as share their keys, at least one token
-        p.heads = mv.g < per_cta ? mv.g : per_cta;
-        p.tok = per_cta / p.heads;
-        p.chunks = (mv.g + p.heads - 1) / p.heads;
-        tiles = (bv.max_q + p.tok - 1) / p.tok;
-        units = (int64_t)mv.L * mv.Hkv * p.chunks;
-        const bool fits = (int64_t)bv.max_q * mv.g * 2 <= per_cta, idle = key_tiles <= 4 && units * tiles * bv.batch < ctx.sm_count / 4;
-        if (per_cta == 16 || !(fits || idle)) break;
-    }
-    p.row_tiles = (int)tiles;
-    const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
-    int splits = attend_splits(units * tiles * bv.batch, ctx.sm_count, key_tiles, 2);
-    while (splits > 1 && splits * rows > partial_rows) --splits;
-    p.out.splits = splits;
-    const int64_t ctas = units * splits * tiles;
+    const Plan n = make_plan(ctx, bv, partial_rows);
+    SimtArgs p = {mv, bv, q, ck, cv, hk, hv, out, ctx.d_status, causal, n.heads, n.tok, n.chunks, n.row_tiles, mv.scale * kLog2e};
+    p.out.splits = n.splits;
+    const int64_t ctas = (int64_t)mv.L * mv.Hkv * n.chunks * n.splits * n.row_tiles;
     if (ctas > INT_MAX) return cudaErrorInvalidConfiguration;
     const dim3 grid((unsigned)ctas, bv.batch);
-    cudaError_t e = mv.elem_bytes == 4 ? launch_t<float>(ctx, p, per_cta, grid, stream) : launch_t<__nv_bfloat16>(ctx, p, per_cta, grid, stream);
-    if (e == cudaSuccess && splits > 1) e = launch_merge_splits(ctx, bv, p.out, stream);
+    cudaError_t e = mv.elem_bytes == 4 ? launch_t<float>(ctx, p, n.per_cta, grid, stream) : launch_t<__nv_bfloat16>(ctx, p, n.per_cta, grid, stream);
+    if (e == cudaSuccess && n.splits > 1) e = launch_merge_splits(ctx, bv, p.out, stream);
     return e;
 }
 

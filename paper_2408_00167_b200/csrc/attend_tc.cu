@@ -586,28 +586,59 @@ void choose_splits(int sms, int64_t units, int tiles, int two_tiles, size_t room
     }
 }
 
+struct Plan {
+    int heads, tok, chunks;   // query heads and tokens of a row tile, tiles of heads per KV head
+    int two_tiles, row_tiles; // as in TcArgs
+    bool one_stream;
+    int cluster, splits;      // splits: all of a row's, cluster * clusters
+};
+
+// Host arithmetic on the batch's bounds.  room: partial results that there is place for, in sets of all rows.
+Plan make_plan(const Ctx &ctx, const BatchView &bv, size_t room) {
+    const ModelView &mv = ctx.model;
+    const int sms = ctx.sm_count > 0 ? ctx.sm_count : 148;   // a validation-only context has none
+    Plan n;
+    n.heads = mv.g < kTileRows ? mv.g : kTileRows;
+    n.tok = kTileRows / n.heads;
+    n.chunks = (mv.g + n.heads - 1) / n.heads;
+    // Two row tiles to a CTA, unless that leaves more than half of the SMs without one.
+    const int64_t units = (int64_t)mv.L * mv.Hkv * n.chunks, one_tile = units * bv.batch * ((bv.max_q + n.tok - 1) / n.tok);
+    n.two_tiles = bv.max_q > n.tok && 2 * one_tile > sms;
+    const int key_tiles = (bv.max_cache + kTileRows - 1) / kTileRows + (bv.max_chunk + kTileRows - 1) / kTileRows;
+    // One row tile to a CTA, two CTAs to an SM, where the keys are few, or not many and every SM has work (rows of 32 KV heads: 16 requests
+    // of up to 512 66 us with two streams to a CTA, 51 with one; 64 of up to 64 97 and 48; 512 rows 15.9 and 14.3; but 64 rows of 4 requests
+    // over 4160 keys 38 and 51, 1024 rows over 5120 87 and 90, 8192 rows of 8 KV heads 463 and 471)
+    n.one_stream = key_tiles <= kFewTiles || (key_tiles <= kManyTiles && one_tile > sms);
+    const int per_cta = n.two_tiles && !n.one_stream ? 2 * n.tok : n.tok;
+    n.row_tiles = (bv.max_q + per_cta - 1) / per_cta;
+    n.cluster = n.splits = 1;
+    if (!n.one_stream) choose_splits(sms, units * n.row_tiles * bv.batch, key_tiles, n.two_tiles, room, n.cluster, n.splits);
+    return n;
+}
+
+size_t room_for(const ModelView &mv, const BatchView &bv, size_t partial_rows) {
+    const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
+    return partial_rows / (rows > 0 ? rows : 1);
+}
+
 }  // namespace
 
 bool attend_tc_supported(const Ctx &ctx) { return ctx.cfg.dtype == FINCH_BF16 && ctx.model.d <= 128; }
+
+void attend_tc_plan(const Ctx &ctx, const BatchView &bv, size_t partial_rows, int &path, int &cluster, int &clusters) {
+    const Plan n = make_plan(ctx, bv, room_for(ctx.model, bv, partial_rows));
+    path = n.one_stream ? FINCH_ATTEND_ONE_STREAM : (n.two_tiles ? FINCH_ATTEND_ROW_PAIRS : FINCH_ATTEND_KEY_PAIRS);
+    cluster = n.cluster;
+    clusters = n.splits / n.cluster;
+}
 
 cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorView &ck, const TensorView &cv, const TensorView &hk,
                              const TensorView &hv, const BatchView &bv, int causal, AttendOut out, size_t partial_rows, cudaStream_t stream) {
     if (bv.batch == 0 || bv.max_q == 0) return cudaSuccess;
     const ModelView &mv = ctx.model;
-    TcArgs p = {mv, bv, out, ctx.d_status, causal, 0, 0, 0, 0, 0, 1, mv.scale * kLog2e};
-    p.heads = mv.g < kTileRows ? mv.g : kTileRows;
-    p.tok = kTileRows / p.heads;
-    p.chunks = (mv.g + p.heads - 1) / p.heads;
-    // Two row tiles to a CTA, unless that leaves more than half of the SMs without one.
-    const int64_t units = (int64_t)mv.L * mv.Hkv * p.chunks, one_tile = units * bv.batch * ((bv.max_q + p.tok - 1) / p.tok);
-    p.two_tiles = bv.max_q > p.tok && 2 * one_tile > ctx.sm_count;
-    const int key_tiles = (bv.max_cache + kTileRows - 1) / kTileRows + (bv.max_chunk + kTileRows - 1) / kTileRows;
-    // One row tile to a CTA, two CTAs to an SM, where the keys are few, or not many and every SM has work (rows of 32 KV heads: 16 requests
-    // of up to 512 66 us with two streams to a CTA, 51 with one; 64 of up to 64 97 and 48; 512 rows 15.9 and 14.3; but 64 rows of 4 requests
-    // over 4160 keys 38 and 51, 1024 rows over 5120 87 and 90, 8192 rows of 8 KV heads 463 and 471)
-    const bool one_stream = key_tiles <= kFewTiles || (key_tiles <= kManyTiles && one_tile > ctx.sm_count);
-    const int per_cta = p.two_tiles && !one_stream ? 2 * p.tok : p.tok;
-    p.row_tiles = (bv.max_q + per_cta - 1) / per_cta;
+    const Plan n = make_plan(ctx, bv, room_for(mv, bv, partial_rows));
+    TcArgs p = {mv, bv, out, ctx.d_status, causal, n.heads, n.tok, n.chunks, n.row_tiles, n.two_tiles, n.cluster, mv.scale * kLog2e};
+    p.out.splits = n.splits;
     Maps maps;
     if (!make_q_map(&maps.q, q, mv.d, bv.total_q, mv.Hq, mv.L, p.tok, p.heads)) return cudaErrorNotSupported;
     // an absent tensor holds no tile; its map is never used
@@ -620,13 +651,11 @@ cudaError_t launch_attend_tc(const Ctx &ctx, const TensorView &q, const TensorVi
         return cudaErrorNotSupported;
     if (!cache) maps.ck = maps.cv = maps.q;
     if (!chunk) maps.hk = maps.hv = maps.q;
-    const size_t rows = (size_t)mv.L * mv.Hq * bv.total_q;
-    if (!one_stream) choose_splits(ctx.sm_count, units * p.row_tiles * bv.batch, key_tiles, p.two_tiles, partial_rows / (rows > 0 ? rows : 1), p.cluster, p.out.splits);
-    const int64_t ctas = units * p.out.splits * p.row_tiles;
+    const int64_t ctas = (int64_t)mv.L * mv.Hkv * n.chunks * n.splits * n.row_tiles;
     if (ctas > INT_MAX) return cudaErrorInvalidConfiguration;
     const dim3 grid((unsigned)ctas, bv.batch);
     cudaError_t e;
-    if (one_stream)
+    if (n.one_stream)
         e = mv.d <= 64 ? launch<64, 1>(ctx, maps, p, grid, stream) : launch<128, 1>(ctx, maps, p, grid, stream);
     else
         e = mv.d <= 64 ? launch<64, 2>(ctx, maps, p, grid, stream) : launch<128, 2>(ctx, maps, p, grid, stream);

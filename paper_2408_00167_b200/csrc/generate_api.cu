@@ -164,6 +164,22 @@ finch_status finch_attend_workspace_bytes(const finch_ctx *ctx, const finch_batc
     return FINCH_OK;
 }
 
+finch_status finch_attend_plan(const finch_ctx *ctx, const finch_batch *batch, int32_t *path, int32_t *cluster, int32_t *splits) {
+    if (!path) return FINCH_ERR_INVALID_ARG;
+    finch_status s = check_batch(ctx, batch);
+    if (s) return s;
+    const size_t rows = attend_ws(ctx, batch->total_q).rows;
+    int c = 1, n = 1;
+    *path = FINCH_ATTEND_MULTIPLY_ADD;
+    if (attend_tc_supported(*ctx))
+        attend_tc_plan(*ctx, view_of(batch), rows, *path, c, n);
+    else
+        n = attend_simt_splits(*ctx, view_of(batch), rows);
+    if (cluster) *cluster = c;
+    if (splits) *splits = n;
+    return FINCH_OK;
+}
+
 finch_status finch_attend(finch_ctx *ctx, const finch_tensor *q, const finch_tensor *cache_k, const finch_tensor *cache_v,
                           const finch_tensor *chunk_k, const finch_tensor *chunk_v, const finch_batch *batch, int32_t causal,
                           const finch_tensor *out, float *row_lse, void *ws, size_t ws_bytes, void *cuda_stream) {

@@ -478,3 +478,34 @@ def test_a_cache_keeps_what_another_stream_reads(lib, monkeypatch):
         for t in (cache._add.new_off, cache._add.len, cache._see.q_off, cache._see.len, cache._ws, cache.table, *cache._tensors):
             assert t.data_ptr() in pointers
     cache.close()
+
+
+def test_attend_plan(lib):
+    """How a batch is shared out, on 148 SMs: the sizes at which the rule changes its mind, and its refusals."""
+    ONE, ROWS, KEYS = fb.FINCH_ATTEND_ONE_STREAM, fb.FINCH_ATTEND_ROW_PAIRS, fb.FINCH_ATTEND_KEY_PAIRS
+
+    def plan(Hq, Hkv, rows, cache, chunk, batch=1, d=128, dtype=fb.FINCH_BF16):
+        c = fb.finch_ctx_create(1, Hq, Hkv, d, dtype, max_batch=batch, max_prompt=rows, max_candidates=cache + chunk, device=-1)
+        try:
+            off = lambda n: [n * i for i in range(batch + 1)]
+            return fb.finch_attend_plan(c, fb.make_batch(off(rows), off(chunk), off(cache), [cache] * batch, [cache] * batch, device="cpu"))
+        finally:
+            fb.finch_ctx_destroy(c)
+
+    assert plan(32, 32, 300, 340, 300) == (ROWS, 1, 1) and plan(32, 32, 300, 256, 300) == (ONE, 1, 1)      # six key tiles, five
+    assert plan(32, 32, 300, 768, 300) == (ROWS, 1, 1) and plan(32, 32, 300, 896, 300) == (ROWS, 2, 1)     # nine, ten
+    assert plan(32, 32, 600, 1024, 600) == (ONE, 1, 1)                                                     # 160 row tiles
+    assert plan(32, 32, 600, 3456, 600) == (ONE, 1, 1) and plan(32, 32, 600, 3457, 600) == (ROWS, 1, 1)    # 32 key tiles, 33
+    assert plan(32, 8, 128, 2048, 128) == (KEYS, 4, 1)
+    assert plan(32, 8, 32, 8192, 32)[:2] == (KEYS, 4) and plan(32, 8, 32, 8192, 32)[2] > 1
+    assert plan(8, 8, 8192, 0, 8192) == (ROWS, 1, 1)
+    assert plan(32, 8, 128, 2048, 128, d=160)[:2] == (fb.FINCH_ATTEND_MULTIPLY_ADD, 1)
+    assert plan(8, 8, 16, 0, 16, dtype=fb.FINCH_F32) == (fb.FINCH_ATTEND_MULTIPLY_ADD, 1, 1)
+    assert plan(8, 8, 16, 500, 16, dtype=fb.FINCH_F32)[2] > 1
+    c = fb.finch_ctx_create(1, 8, 8, 64, fb.FINCH_BF16, device=-1)
+    b, out = _batch(B=1), C.c_int32()
+    assert lib.finch_attend_plan(c, C.addressof(b), None, None, None) == INVALID
+    assert lib.finch_attend_plan(c, None, C.addressof(out), None, None) == INVALID
+    assert lib.finch_attend_plan(c, C.addressof(b), C.addressof(out), None, None) == OK
+    assert lib.finch_attend_plan(c, C.addressof(_batch(B=0, q=0, m=0, c=0, max_q=0, max_m=0, max_c=0)), C.addressof(out), None, None) == OK
+    fb.finch_ctx_destroy(c)
