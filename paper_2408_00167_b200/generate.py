@@ -55,8 +55,11 @@ class PagedCache:
         self._ctx_all = fb.finch_ctx_create(n_layers, n_q_heads, n_kv_heads, head_dim, dtype, scale=scale, **bounds)
         self._ctx = fb.finch_ctx_create(1, n_q_heads, n_kv_heads, head_dim, dtype, scale=scale, **bounds)
         self.len = np.zeros(batch, dtype=np.int32)
-        self._add = self._see = self._ws = None
+        self._add = self._see = None
+        self._ws = torch.empty(fb.finch_pages_workspace_bytes(self._ctx, fb.make_paged_batch(self.len, device="cpu")),
+                               dtype=torch.uint8, device=device)
         self._made_on = self._step_on = self._stream()   # the streams that the arrays above and a step's description belong to
+        self._readers = set()                            # other streams that have read the arrays above
         self._steps, self._has = 0, [0] * n_layers      # steps since the cache was filled, and those whose rows a layer has
 
     def close(self) -> None:
@@ -103,8 +106,6 @@ class PagedCache:
         self.len = self.len + np.int32(tokens)
         self._see = fb.make_paged_batch(self.len, q_off=off, device=self.device)
         self._steps += 1
-        if self._ws is None:
-            self._ws = self.torch.empty(fb.finch_pages_workspace_bytes(self._ctx, self._see), dtype=self.torch.uint8, device=self.device)
 
     def _stream(self):
         return fb._stream(None) if self.device.type == "cuda" else None
@@ -112,12 +113,15 @@ class PagedCache:
     def _read_here(self, batch, made_on) -> None:
         """A step's description is replaced by the next one's, and everything goes when the cache does: memory that the current stream's
         kernels read, where it was allocated for another stream, waits for them before it serves another purpose."""
-        if self._stream() == made_on == self._made_on:
-            return
-        stream = self.torch.cuda.current_stream()
-        for t in (*self._tensors, self.table, self.slot, self._ws, batch.q_off, batch.new_off, batch.len):
+        now, held = self._stream(), ()
+        if now != made_on:
+            held = batch.q_off, batch.new_off, batch.len
+        if now != self._made_on and now not in self._readers:      # once is for good
+            self._readers.add(now)
+            held += *self._tensors, self.table, self.slot, self._ws
+        for t in held:
             if t is not None:
-                t.record_stream(stream)
+                t.record_stream(self.torch.cuda.current_stream())
 
     def _check_rows(self, what: str, t, heads: int) -> None:
         if t.shape != (1, heads, self._add.c.total_new, self.d):

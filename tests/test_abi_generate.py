@@ -470,13 +470,15 @@ def test_a_cache_keeps_what_another_stream_reads(lib, monkeypatch):
 
     cache.step()
     assert not both()
-    for made, read in (("a", "b"), ("b", "a"), ("b", "b")):
+    lasting, seen = (cache._ws, cache.table, cache.slot, *cache._tensors), {"a"}
+    for made, read in (("a", "b"), ("b", "a"), ("b", "b"), ("c", "c"), ("a", "c"), ("a", "a")):
         now[0] = made
         cache.step()
         now[0] = read
-        pointers = {p for p, s in both() if s == read}
-        for t in (cache._add.new_off, cache._add.len, cache._see.q_off, cache._see.len, cache._ws, cache.table, *cache._tensors):
-            assert t.data_ptr() in pointers
+        want = [] if made == read else [cache._add.new_off, cache._add.len, cache._see.q_off, cache._see.len]
+        want += [] if read in seen else lasting          # for good
+        seen.add(read)
+        assert sorted(both()) == sorted((t.data_ptr(), read) for t in want)
     cache.close()
 
 
