@@ -415,9 +415,10 @@ def _array(what: str, t, dtype, like, shape):
     return t.data_ptr() or None
 
 
-def _rows_of(what: str, t, dtype, like, n: int, dense: bool) -> None:
-    """An array of the batch description: n entries, or (not dense: one for each row) at least so many."""
-    if t.dtype != dtype or t.get_device() != like.get_device() or not t.is_contiguous() or t.numel() < n or (dense and t.numel() != n):
+def _rows_of(what: str, t, dtype, like, n: int) -> None:
+    """An array of the batch description: n entries, or at least so many where it has one axis (more axes of other sizes would be read
+    with the wrong pitch)."""
+    if t.dtype != dtype or t.get_device() != like.get_device() or not t.is_contiguous() or t.numel() < n or (t.dim() > 1 and t.numel() != n):
         raise ValueError(f"{what}: expected {n} contiguous {dtype} on {like.device}, got {t.dtype} of {tuple(t.shape)} on {t.device}")
 
 
@@ -524,9 +525,9 @@ def finch_attend(ctx, q, cache_k, cache_v, chunk_k, chunk_v, batch: Batch, out, 
     if batch.q_off.get_device() != q.get_device():
         raise ValueError(f"finch_attend: the batch description is on {batch.q_off.device}, the tensors on {q.device}")
     if batch.prompt_self_lse is not None:
-        _rows_of("finch_attend: prompt_self_lse", batch.prompt_self_lse, f32, q, L * Hq * rows, True)
+        _rows_of("finch_attend: prompt_self_lse", batch.prompt_self_lse, f32, q, L * Hq * rows)
     if batch.row_limit is not None:
-        _rows_of("finch_attend: row_limit", batch.row_limit, _dtypes_of()[0], q, rows, False)
+        _rows_of("finch_attend: row_limit", batch.row_limit, _dtypes_of()[0], q, rows)
     z = _VIEW_BYTES
     ws, ws_bytes = _space("finch_attend", ws, q)
     _check(load().finch_attend(ctx, v, v + z, v + 2 * z, v + 3 * z, v + 4 * z, C.addressof(c), 1 if causal else 0, v + 5 * z,

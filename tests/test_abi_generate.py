@@ -341,6 +341,7 @@ def test_the_binding_refuses_tensors_that_do_not_hold_the_call(lib, ctx, monkeyp
     padded = dict(attend, q=bf(2, 8, 9, 64), out=bf(2, 8, 9, 64), cache_k=bf(2, 2, 9, 64), chunk_v=bf(2, 2, 8, 64))
     refused(fb.finch_attend, padded, row_lse=[torch.zeros(2, 8, 9)])
     refused(fb.finch_attend, dict(attend, batch=limited(prompt_self_lse=torch.zeros(2, 8, 5), row_limit=i32(1, 2, 3, 4, 5, 6))))
+    refused(fb.finch_attend, dict(attend, batch=limited(prompt_self_lse=torch.zeros(200))))         # one axis: a buffer that holds them
 
     def pages(L=2, Hkv=2, d=64, requests=2, dtype=torch.bfloat16):
         pool, scale = (lambda: torch.zeros((L, 3, Hkv, 64, d), dtype=torch.uint8)), (lambda: torch.zeros((L, 3, Hkv)))
