@@ -365,7 +365,8 @@ typedef struct {
     const int32_t *q_off;    /* device, [batch+1]: query rows (finch_pages_attend; else not read)                          */
     const int32_t *new_off;  /* device, [batch+1]: new rows (finch_pages_append; else not read)                            */
     const int32_t *len;      /* device, [batch]: tokens in the cache; for the append, before it                            */
-    int32_t total_q, total_new, max_q, max_new, max_len; /* host copies and upper bounds                                   */
+    int32_t total_q, total_new, max_q, max_new, max_len; /* host copies and upper bounds; max_len + max_new (append) within the context's
+                                                            max_candidates, its full pages within the table's width          */
 } finch_paged_batch;
 
 /* Appends rows [new_off[b], new_off[b+1]) of new_k / new_v ([n_layers][n_kv_heads][total_new][head_dim]) behind each request's len[b]
@@ -381,7 +382,7 @@ finch_status finch_pages_append(finch_ctx *ctx, const finch_pages *pages, const 
  * len[b] - n_q + i + 1.  Made for the last token, or the last few; every 8 rows of a KV head (its query heads times tokens)
  * read the cache once.  Pages may be shared between requests.  A page number outside [0, n_pages) sets
  * FINCH_DEV_BAD_INDEX and its tokens count as not there.  row_lse may be NULL.  A V row that is not finite may reach rows of
- * the same 8 that do not see it.
+ * the same 8 that do not see it, and come out as NaN where it is an infinity.
  * Workspace: finch_pages_workspace_bytes, the same for every call of a context (and of every context of its head_dim and device). */
 finch_status finch_pages_workspace_bytes(const finch_ctx *ctx, const finch_paged_batch *batch, size_t *out);
 finch_status finch_pages_attend(finch_ctx *ctx, const finch_pages *pages, const finch_paged_batch *batch, const finch_tensor *q,
