@@ -325,7 +325,7 @@ finch_status finch_rotate(finch_ctx *ctx, const finch_tensor *q, const finch_ten
  * A row that sees nothing gives zeros and a log-sum-exp of -inf.  prompt_self_lse adds its term to the denominator (and to row_lse),
  * as in finch_score.  `out` has q's shape and any strides; it must not overlap an input.  row_lse may be NULL; it must not overlap prompt_self_lse.  budget is not read;
  * row_norm must be 0 (`budget` may hold anything, but not be NULL).  bf16 with head_dim <= 128 runs on the tensor cores (P = exp(..) is rounded to bf16 there), everything else in
- * fp32 multiply-adds.  What a row does not see is not read into its result where it lies behind the request's last candidate;
+ * fp32 multiply-adds.  What a row does not see is not read into its result where it lies behind the request's last candidate or every row's limit;
  * a V row that is not finite, but is seen by some row of a request, may make rows before it not finite on the tensor cores.
  * Workspace: finch_attend_workspace_bytes, enough for every batch with no larger total_q. */
 finch_status finch_attend_workspace_bytes(const finch_ctx *ctx, const finch_batch *batch, size_t *out);

@@ -15,8 +15,8 @@
 // Order.  One thread issues S(s, i+1) behind P V (s, i): the completion of S then says that O is at rest, and the softmax warps
 // may scale it.  They do so only when a row's maximum has grown by more than 2^8: until then P is taken against the old reference.
 //
-// A masked key has P = 0, but zero times a NaN or infinity is none: rows of V behind the last candidate are cleared before
-// they are multiplied.
+// A masked key has P = 0, but zero times a NaN or infinity is none: rows of V behind the last candidate, and behind the last that a
+// row of the CTA sees where there are row limits, are cleared before they are multiplied.
 #include "attend.cuh"
 
 namespace finch {
@@ -180,6 +180,13 @@ attend_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TcAr
     const int all0 = tiles_for(limit_s[0]), all1 = STREAMS == 2 ? tiles_for(limit_s[1]) : 0, all = max(all0, all1);
     const int begin = (int)((int64_t)all * split / p.out.splits), end = (int)((int64_t)all * (split + 1) / p.out.splits);
     const int n_tiles = end - begin;                    // loaded
+    // What a key tile holds for this CTA: with row limits, candidates behind the largest of its rows' may be memory that nobody has
+    // written, like those behind the request's last.
+    UnitInfo held = u;
+    if (p.bv.row_limit) {
+        const int most = STREAMS == 2 ? max(limit_s[0], limit_s[1]) : limit_s[0];
+        held.c = min(u.c, most), held.m = max(0, most - u.c);
+    }
     int count[2];                                        // of each stream
     if (STREAMS == 1) {
         count[0] = n_tiles, count[1] = 0;
@@ -202,7 +209,7 @@ attend_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TcAr
             uint32_t ph = 1;   // of the slot's last reader: the first round waits for nobody
             bool ok = true;
             for (int t = 0; t < n_tiles && ok; ++t) {
-                const KeyTile kt = key_tile(u, begin + t);
+                const KeyTile kt = key_tile(held, begin + t);
                 for (int v = 0; v < 2; ++v, ++item, slot = slot + 1 == kStages ? (ph ^= 1, 0) : slot + 1) {
                     if (item >= kStages && !(ok = mbar_wait(&bar.empty[slot], ph, &abort_flag))) break;
                     mbar_expect_tx(&bar.full[slot], Lay::kTile);
@@ -228,8 +235,9 @@ attend_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TcAr
             const uint64_t qd0 = smem_desc_sw128(q_u), qd[2] = {qd0, two_tiles ? qd0 + kTile16 : qd0};
             const uint64_t kd = smem_desc_sw128(ring_u), vd = smem_desc_sw128_mn(ring_u, kSlabBytes);
             // the tiles whose V rows are cleared behind the last token: the cache's last, the chunk's last
-            const int ragged0 = u.c % kTileRows ? cache_tiles - 1 - begin : -1;
-            const int ragged1 = u.m % kTileRows ? cache_tiles + (u.m + kTileRows - 1) / kTileRows - 1 - begin : -1;
+            const int held_tiles = (held.c + kTileRows - 1) / kTileRows;
+            const int ragged0 = held.c % kTileRows ? held_tiles - 1 - begin : -1;
+            const int ragged1 = held.m % kTileRows ? held_tiles + (held.m + kTileRows - 1) / kTileRows - 1 - begin : -1;
             const int step = two_tiles || STREAMS == 1 ? 2 : 4;           // items from a stream's tile to its next
             // slot and phase of each stream's next K and V item
             int k_slot[2], v_slot[2], tile_k[2], tile_v[2];
@@ -310,9 +318,9 @@ attend_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TcAr
             for (int s = 0; s < (two_tiles ? 2 : 1); ++s) mbar_wait(&bar.q_full[s], 0, &abort_flag);
         }
     } else if (warp == 2) {
-        // ---------------------------------------------------------------- V rows behind the last candidate
+        // ---------------------------------------------------------------- V rows behind the last candidate that counts
         for (int t = 0; t < n_tiles; ++t) {
-            const KeyTile kt = key_tile(u, begin + t);
+            const KeyTile kt = key_tile(held, begin + t);
             if (kt.valid == kTileRows) continue;
             const int item = 2 * t + 1, slot = item % kStages;
             // this warp has not seen the slot's earlier phases: it waits until the slot is this tile's, then for its bytes

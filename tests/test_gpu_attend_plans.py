@@ -114,6 +114,26 @@ def test_one_stream_over_many_key_tiles(d, reqs):
     _check(Attend(1, 32, 32, d, reqs, slack=5), [0, 31], (ONE, 1, 1))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,req,plan,most", [
+    (2, 1, (40, 130, 40), (ONE, 1, 1), [100, 128, 130, 131, 1, 0]),
+    (32, 32, (300, 500, 300), (ROWS, 1, 1), [300, 500, 501, 690]),
+    (32, 32, (300, 1100, 300), (ROWS, 2, 1), [1000, 1101]),
+    (4, 1, (20, 900, 20), (KEYS, 4, 1), [70, 899, 910]),
+    (4, 1, (3, 8000, 3), (KEYS, 4, 8), [7900, 64]),
+    (32, 32, (600, 1000, 600), (ONE, 1, 1), [999, 1333]),
+])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_candidates_that_no_row_sees_may_hold_anything(dtype, d, Hq, Hkv, req, plan, most):
+    """Row limits that end in front of the last candidate: K and V behind the largest are NaN, as memory that nobody has written."""
+    n, c, m = req
+    for top in most:
+        a = Attend(1, Hq, Hkv, d, [req], dtype=dtype, limits=[top if i % 5 == 3 else max(0, top - i % 67) for i in range(n)])
+        a.ck[:, :, top:c] = a.cv[:, :, top:c] = math.nan
+        a.hk[:, :, max(0, top - c):] = a.hv[:, :, max(0, top - c):] = math.nan
+        _check(a, [0, Hq - 1], plan if dtype == "bf16" else None, dtype == "bf16")
+
+
 def test_plans_of_few_keys():
     """Up to five key tiles a CTA has one stream; the tests of the tiles' edges take it."""
     a = Attend(1, 32, 32, 64, [(200, 300, 200)])
